@@ -51,7 +51,9 @@ typedef enum {
   SPT_HASHED = 5      /* segment of width M (=W) of an open-addressed table   */
 } spt_level_kind;
 
-typedef enum { SPT_F32 = 0, SPT_F64 = 1 } spt_dtype;
+/* The values of tensors and of their dense operands are SPT_F32 or SPT_F64. The operations on a cache of
+ * keys and values and on logits (below) take SPT_F32, SPT_F16 and SPT_BF16. */
+typedef enum { SPT_F32 = 0, SPT_F64 = 1, SPT_F16 = 2, SPT_BF16 = 3 } spt_dtype;
 
 /* Level properties that are configurable per level (Section 3.3, Table 1).
  * full / branchless / compact follow from the kind. */
@@ -438,6 +440,158 @@ spt_status spt_add_to_dense(const spt_tensor* B, const spt_tensor* C, void* A, i
  */
 enum { SPT_BAD_POS = 1, SPT_BAD_POS_END = 2, SPT_BAD_CRD = 4, SPT_BAD_ORDER = 8, SPT_BAD_OFFSET = 16 };
 spt_status spt_validate(const spt_tensor* T, int32_t* err_dev, void* stream);
+
+/*
+ * A paged cache of keys and values, and attention over it.
+ *
+ * The keys of a cache are a tensor K(row, token, head, d): `rows` sequences whose tokens lie in pages of
+ * `page` slots anywhere in a pool, as the levels (dense rows, dense places of a row's table, singleton
+ * pages, dense slots, dense heads, dense width). Row s holds len[s] tokens; its table row
+ * table[s*row_pages ..] names the pages of tokens 0 .. page-1, page .. 2*page-1, and so on. As with ELL, a
+ * negative page number is padding: the tokens of a table entry outside [0, pages) count as absent (never
+ * read, written or attended to), and table entries behind the row's last page are not looked at. Numbers in
+ * len below 0 count as 0, above page*row_pages as that.
+ * refs[p] = number of table rows that list page p; a page with refs 0 is free. Pages are shared by forking; a
+ * shared page is read by several rows and, through the entry points here, written by none.
+ * The V pool has the layout of the K pool: value d of (layer l, page p, slot o, head h) is element
+ * l*layer_stride + p*page_stride + o*slot_stride + h*head_stride + d.
+ *
+ *   dtype      SPT_F32, SPT_F16 or SPT_BF16; of K, V and of every k, v, q and out below
+ *   layers     >= 1; the layers share table, len and refs
+ *   heads      >= 1, of K and V
+ *   width      values of a head: a multiple of 8, 8 .. 256
+ *   page       slots of a page: a power of two, 1 .. 65536
+ *   rows       <= 2^20; row_pages: places of a row of the table
+ *   pages      < 2^31 - 1; rows * (row_pages + 1) < 2^31 - 1; page * row_pages < 2^31 - 65537
+ *   strides    in elements, not negative, multiples of 16 bytes; K and V are 16-byte aligned
+ * table, len and refs are read and written by the entry points that say so; the struct itself is read only
+ * during the call, on the host. Like every call they enqueue kernels and return; all sizes that change from
+ * step to step are on the device, so a step can be captured in a graph and replayed.
+ *
+ * `first` (device, rows + 1 entries, ascending from 0, as pos of a compressed level): the last
+ * n = first[s+1] - first[s] tokens of row s are drafted ones, described by rows first[s] .. first[s+1]-1 of
+ * k, v, q, out, tree. Rows from first[rows] on are left as they were. Offsets count as cut to [0, T].
+ *
+ * Patterns (tree, keep; seen below) are CSR matrices whose values are not read: dtype is ignored, vals may
+ * be NULL, nvals is the number of entries. Entries outside the ranges named are skipped.
+ */
+typedef struct {
+  int32_t dtype;
+  int32_t layers;
+  int32_t heads;
+  int32_t width;
+  int32_t page;
+  int32_t rows;
+  int32_t row_pages;
+  int32_t reserved;
+  int64_t pages;
+  int64_t layer_stride;
+  int64_t page_stride;
+  int64_t slot_stride;
+  int64_t head_stride;
+  void* K;
+  void* V;
+  int32_t* table;
+  int32_t* len;
+  int32_t* refs;
+} spt_cache;
+
+/*
+ * spt_cache_extend: makes room for add[s] (device, rows entries; <= 0: none) more tokens in row s: its table
+ * receives the pages that are needed, len[s] += add[s]. The append of Table 3: pages are taken from the free
+ * ones, the lowest numbers first, rows in their order, so the result does not depend on timing. If tokens are
+ * to go into a partly filled last page that other rows list too, the row first receives a page of its own
+ * (copy on write): the filled slots are copied in all layers and the shared page's refs fall by one, for
+ * every such row. Pages that become free in a call are taken by a later one.
+ * A row whose tokens would not fit into its table is refused and left as it was; once the free pages do not
+ * suffice for a row, that row and all later ones that need a page are refused. *refused_dev (device int32)
+ * receives the number of rows refused. Workspace: SPT_CACHE_EXTEND.
+ *
+ * spt_cache_write: writes the drafted tokens' k and v into their slots of one layer. Token i of the call,
+ * head h: k[i*token_stride + h*head_stride ..][width], v alike (strides in elements, multiples of 16 bytes, both
+ * pointers 16-byte aligned). T <= 2^24: rows of k and v.
+ *
+ * spt_cache_compact: keeps some of the drafted tokens: keep is a pattern, rows x (drafted tokens of a row),
+ * ordered and unique; row s lists the ones to keep, counted within the row. In all layers they are drawn
+ * together behind the tokens before them, len[s] is cut to them and pages behind are given back. Rows with
+ * n = 0 are left as they were, rows of which nothing is kept lose all n. The slots written to must not lie in
+ * pages that other rows list (they do not between spt_cache_extend and the next spt_cache_fork).
+ *
+ * spt_cache_free: cuts row s to new_len[s] tokens (device; 0 empties it; negative or beyond len[s]: left as it
+ * is) and gives the pages behind back: their refs fall by one, their table entries become -1.
+ *
+ * spt_cache_fork: row children[i] (device, n entries) becomes a copy of row parents[i] that shares its pages;
+ * what it held before is given back. One parent may have many children. Entries with rows outside
+ * [0, rows), with a child that is a parent in the call too, and with a child that a later entry names
+ * again are skipped. n <= 65536.
+ */
+spt_status spt_cache_extend(const spt_cache* c, const int32_t* add, int32_t* refused_dev, void* ws, size_t ws_bytes,
+                            void* stream);
+spt_status spt_cache_write(const spt_cache* c, int32_t layer, const int32_t* first, int64_t T, const void* k,
+                           const void* v, int64_t token_stride, int64_t head_stride, void* stream);
+spt_status spt_cache_compact(const spt_cache* c, const int32_t* first, const spt_tensor* keep, void* stream);
+spt_status spt_cache_free(const spt_cache* c, const int32_t* new_len, void* stream);
+spt_status spt_cache_fork(const spt_cache* c, int64_t n, const int32_t* parents, const int32_t* children, void* stream);
+
+/*
+ * Attention of the drafted tokens over their row's tokens, in one layer: a product sampled at a sparse pattern,
+ * a softmax over each row's stored entries, and a sparse x dense product, in one pass over the cache.
+ * Drafted token i (of row s, with n drafted tokens) sees all tokens of the row before the drafted ones, and the
+ * drafted tokens j that row i of `tree` lists (a pattern, T x (drafted tokens of a row), columns counted within
+ * the row, in any order, repeated ones count once); tree NULL: those up to itself.
+ *   z_t = scale * sum_d q(i,h,d) K(t, h / (q_heads/heads), d),  p_t = exp(z_t) / sum of exp(z) over the tokens seen,
+ *   out(i,h,:) = sum_t p_t V(t, h / (q_heads/heads), :),        lse(i,h) = ln(sum of exp(z)).
+ * A token that sees nothing (or only scores of -infinity) gets out = 0 and lse = -infinity. What a token
+ * does not see does not reach it, infinities and NaNs in K and V included. Scores, sums and out are held in
+ * 32 bits; SPT_F16 and SPT_BF16 multiply in matrix instructions on values of that type, for which exp(z - max)
+ * is rounded to it.
+ * q, out: T x q_heads x width with the strides given (elements, multiples of 16 bytes; pointers 16-byte aligned),
+ * T <= 2^24; q_heads a multiple of heads; lse (may be NULL): float, T x q_heads. The query of the workspace knows no lengths;
+ * its size does not depend on T. The same call gives the same bits. Workspace: SPT_CACHE_ATTENTION.
+ */
+spt_status spt_cache_attention(const spt_cache* c, int32_t layer, const int32_t* first, int64_t T,
+                               const spt_tensor* tree, const void* q, int32_t q_heads, int64_t q_token_stride,
+                               int64_t q_head_stride, float scale, void* out, int64_t out_token_stride,
+                               int64_t out_head_stride, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+typedef enum { SPT_CACHE_EXTEND = 0, SPT_CACHE_ATTENTION = 1 } spt_cache_op;
+/* Workspace size in bytes (q_heads only for SPT_CACHE_ATTENTION). 0 for an invalid cache, else >= 256. */
+size_t spt_cache_workspace_bytes(int32_t op, const spt_cache* c, int32_t q_heads);
+
+/*
+ * Rules on logits: out = logits changed by penalties for repeated tokens, then biases, then a mask. A dense
+ * result from a dense and several sparse operands, in one pass.
+ * Row r of the R x V matrix belongs to sequence s with first[s] <= r < first[s+1] (first as above, `sequences` + 1
+ * entries; NULL: R = sequences, row r is sequence r). Rows from first[sequences] on are left as they were.
+ * With c = number of times that token v is counted for row r,
+ *   x = logits(r,v);  if c > 0: x = (x > 0 ? x / repetition[s] : x * repetition[s]) - (presence[s] + frequency[s] * c);
+ *   x += bias(s,v) where stored;  x = -infinity where not allowed.
+ * Computed in 32 bits, rounded once to dtype.
+ *   seen        pattern, sequences x V, any order: each entry counts once (repeated ones again); NULL: none
+ *   drafts      device int32, R: the token of row r; NULL: none. Those on row r's way count too: the entries of row
+ *               r of `tree` (a pattern, R x (rows of a sequence), columns counted within the sequence), or, tree
+ *               NULL, those of its sequence's rows up to r. A token that lies on the way twice counts twice.
+ *   repetition, presence, frequency   device float, one per sequence; NULL: 1, 0, 0
+ *   bias        CSR, sequences x V, SPT_F32, columns unique in a row; NULL: none
+ *   allowed     device uint32, R rows of allowed_stride words: bit v % 32 of word v / 32; NULL: all are
+ * logits and out may be the same array. dtype SPT_F32, SPT_F16 or SPT_BF16; row strides in elements, >= V;
+ * V < 2^31 - 1, R and sequences <= 2^24. Needs no workspace.
+ */
+typedef struct {
+  const int32_t* first;
+  int64_t sequences;
+  const spt_tensor* seen;
+  const spt_tensor* tree;
+  const int32_t* drafts;
+  const float* repetition;
+  const float* presence;
+  const float* frequency;
+  const spt_tensor* bias;
+  const uint32_t* allowed;
+  int64_t allowed_stride;
+} spt_logit_rules;
+spt_status spt_adjust_logits(int32_t dtype, int64_t R, int64_t V, const void* logits, int64_t logits_stride,
+                             const spt_logit_rules* rules, void* out, int64_t out_stride, void* stream);
 
 /* Workspace size in bytes for `op` on tensor T (J only for MTTKRP and TTM).
  * Returns 0 for invalid descriptors (spt_last_error says why). Never fails for

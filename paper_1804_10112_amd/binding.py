@@ -22,14 +22,17 @@ SPT_OP_TO_CSF, SPT_OP_TO_ELL, SPT_OP_DIA_OFFSETS, SPT_OP_TO_COO = 6, 7, 8, 9
 SPT_OP_SPMV_SPARSE_X, SPT_OP_SPDM = 10, 11
 SPT_ORDER_ROW_COL, SPT_ORDER_ROW_STABLE = 0, 1
 SPT_ORDERED, SPT_UNIQUE = 1, 2
-SPT_F32, SPT_F64 = 0, 1
+SPT_F32, SPT_F64, SPT_F16, SPT_BF16 = range(4)
+SPT_CACHE_EXTEND, SPT_CACHE_ATTENTION = 0, 1
 SPT_STATIC_SCRATCH_BYTES = 4 << 20
 
 SYMBOLS = ["spt_spmv", "spt_coo_to_csr", "spt_ttv", "spt_mttkrp", "spt_workspace_bytes",
            "spt_last_error", "spt_version", "spt_probe_read", "spt_probe_gather",
            "spt_spmv_sparse_x", "spt_spdm", "spt_innerprod", "spt_ttm",
            "spt_add", "spt_mul", "spt_add_workspace_bytes", "spt_mul_dense", "spt_add_to_dense", "spt_coo3_to_csf", "spt_to_ell",
-           "spt_coo_dia_offsets", "spt_coo_to_dia", "spt_to_coo", "spt_to_hashed_rows", "spt_spmv_static", "spt_validate"]
+           "spt_coo_dia_offsets", "spt_coo_to_dia", "spt_to_coo", "spt_to_hashed_rows", "spt_spmv_static", "spt_validate",
+           "spt_cache_extend", "spt_cache_write", "spt_cache_compact", "spt_cache_free", "spt_cache_fork",
+           "spt_cache_attention", "spt_cache_workspace_bytes", "spt_adjust_logits"]
 
 
 class SptLevel(C.Structure):
@@ -43,6 +46,18 @@ class SptTensor(C.Structure):
     _fields_ = [("order", C.c_int32), ("nlevels", C.c_int32), ("dtype", C.c_int32),
                 ("reserved", C.c_int32), ("level", SptLevel * 4), ("vals", C.c_void_p),
                 ("nvals", C.c_int64)]
+
+
+class SptCache(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "layers", "heads", "width", "page", "rows", "row_pages", "reserved")]
+                + [(n, C.c_int64) for n in ("pages", "layer_stride", "page_stride", "slot_stride", "head_stride")]
+                + [(n, C.c_void_p) for n in ("K", "V", "table", "len", "refs")])
+
+
+class SptLogitRules(C.Structure):
+    _fields_ = [("first", C.c_void_p), ("sequences", C.c_int64), ("seen", C.c_void_p), ("tree", C.c_void_p),
+                ("drafts", C.c_void_p), ("repetition", C.c_void_p), ("presence", C.c_void_p), ("frequency", C.c_void_p),
+                ("bias", C.c_void_p), ("allowed", C.c_void_p), ("allowed_stride", C.c_int64)]
 
 
 class SptError(RuntimeError):
@@ -116,6 +131,19 @@ def lib():
         L.spt_probe_read.argtypes = [vp, sz, i32, vp, vp]
         L.spt_probe_gather.restype = i32
         L.spt_probe_gather.argtypes = [vp, C.c_int64, vp, i32, vp, vp]
+        i64 = C.c_int64
+        L.spt_cache_extend.argtypes = [vp, vp, vp, vp, sz, vp]
+        L.spt_cache_write.argtypes = [vp, i32, vp, i64, vp, vp, i64, i64, vp]
+        L.spt_cache_compact.argtypes = [vp, vp, vp, vp]
+        L.spt_cache_free.argtypes = [vp, vp, vp]
+        L.spt_cache_fork.argtypes = [vp, i64, vp, vp, vp]
+        L.spt_cache_attention.argtypes = [vp, i32, vp, i64, vp, vp, i32, i64, i64, C.c_float, vp, i64, i64, vp, vp, sz, vp]
+        L.spt_adjust_logits.argtypes = [i32, i64, i64, vp, i64, vp, vp, i64, vp]
+        for name in ("extend", "write", "compact", "free", "fork", "attention"):
+            getattr(L, "spt_cache_" + name).restype = i32
+        L.spt_adjust_logits.restype = i32
+        L.spt_cache_workspace_bytes.restype = sz
+        L.spt_cache_workspace_bytes.argtypes = [i32, vp, i32]
         _lib = L
     return _lib
 
@@ -143,7 +171,7 @@ def _p(t):
 
 
 def _desc(T):
-    return C.addressof(T.c) if isinstance(T, DeviceTensor) else C.addressof(T)
+    return C.addressof(T.c) if isinstance(T, (DeviceTensor, DeviceCSR, DeviceCache, LogitRules)) else C.addressof(T)
 
 
 _raw_stream = _device = None
@@ -375,3 +403,178 @@ class DeviceTensor:
         import torch
         n = spt_workspace_bytes(op, self, J)
         return torch.empty(n, dtype=torch.uint8, device=self.device)
+
+
+def _invalid(message):
+    raise SptError(SPT_ERR_INVALID_ARG, message)
+
+
+def _dtype_code(dtype):
+    import torch
+    codes = {torch.float32: SPT_F32, torch.float64: SPT_F64, torch.float16: SPT_F16, torch.bfloat16: SPT_BF16}
+    if dtype not in codes:
+        raise TypeError(f"values must be float32, float16 or bfloat16, got {dtype}")
+    return codes[dtype]
+
+
+def _i32(t, count, name):
+    """Device pointer of a contiguous int32 tensor of at least `count` entries (None -> NULL)."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < count:
+        _invalid(f"{name} must be a contiguous int32 tensor of at least {count} entries")
+    return t.data_ptr()
+
+
+def _stride(t, d):
+    """A stride, 0 where it is never used (torch leaves those of a dimension of one or none as they come)."""
+    return t.stride(d) if t.shape[d] > 1 else 0
+
+
+class DeviceCSR:
+    """spt_tensor descriptor of a CSR matrix whose arrays are device tensors already: pos (rows + 1 entries) and crd int32,
+    vals float32 or float64; without vals a pattern."""
+
+    def __init__(self, pos, crd, cols, vals=None, ordered=False, unique=False):
+        rows = pos.numel() - 1
+        t = SptTensor()
+        t.order = t.nlevels = 2
+        t.dtype = SPT_F32 if vals is None else _dtype_code(vals.dtype)
+        t.level[0].kind, t.level[0].mode, t.level[0].N, t.level[0].flags = 0, 0, rows, SPT_ORDERED | SPT_UNIQUE
+        o = t.level[1]
+        o.kind, o.mode, o.N, o.M = 1, 1, int(cols), rows
+        o.flags = (SPT_ORDERED if ordered else 0) | (SPT_UNIQUE if unique else 0)
+        o.pos, o.crd = _i32(pos, 1, "pos"), _i32(crd, 0, "crd")
+        if vals is not None and (vals.numel() != crd.numel() or not vals.is_contiguous()):
+            _invalid("vals must be contiguous, one value for each entry of crd")
+        t.vals, t.nvals = _p(vals), crd.numel()
+        self.keep = (pos, crd, vals)
+        self.c = t
+
+
+class DeviceCache:
+    """spt_cache descriptor of device tensors: K and V (layers, pages, slots of a page, heads, width) in any strides with
+    contiguous values of a head, table (rows, pages of a row), len (rows) and refs (pages), int32 and contiguous."""
+
+    def __init__(self, K, V, table, length, refs):
+        import torch
+        if K.dim() != 5 or K.shape != V.shape or K.stride() != V.stride() or K.dtype != V.dtype:
+            _invalid("K and V must be alike: (layers, pages, slots of a page, heads, width)")
+        if K.stride(4) != 1:
+            _invalid("the values of a head must be contiguous")
+        if table.dim() != 2:
+            _invalid("table must be (rows, pages of a row)")
+        c = SptCache()
+        c.dtype = _dtype_code(K.dtype)
+        c.layers, c.pages, c.page, c.heads, c.width = K.shape
+        c.rows, c.row_pages = table.shape
+        c.layer_stride, c.page_stride, c.slot_stride, c.head_stride = (_stride(K, d) for d in range(4))
+        c.K, c.V = K.data_ptr(), V.data_ptr()
+        c.table, c.len, c.refs = _i32(table, 0, "table"), _i32(length, c.rows, "len"), _i32(refs, c.pages, "refs")
+        self.K, self.V, self.table, self.len, self.refs = K, V, table, length, refs
+        self.c = c
+
+    def workspace(self, op, q_heads=0):
+        import torch
+        return torch.empty(spt_cache_workspace_bytes(op, self, q_heads), dtype=torch.uint8, device=self.K.device)
+
+    def _tokens(self, t, name, heads):
+        """(tokens, heads, width) of the cache's dtype: token and head strides."""
+        if t.dtype != self.K.dtype or t.dim() != 3 or t.shape[2] != self.c.width or t.shape[1] != heads or t.stride(2) != 1:
+            _invalid(f"{name} must be (tokens, {heads}, {self.c.width}), {self.K.dtype}, values of a head contiguous")
+        return _stride(t, 0), _stride(t, 1)
+
+
+def spt_cache_workspace_bytes(op, cache, q_heads=0) -> int:
+    n = lib().spt_cache_workspace_bytes(op, _desc(cache), q_heads)
+    if n == 0:
+        raise SptError(SPT_ERR_INVALID_ARG, spt_last_error())
+    return n
+
+
+def spt_cache_extend(cache, add, refused_dev, ws=None, stream=None):
+    p, n = _ws(ws)
+    _check(lib().spt_cache_extend(_desc(cache), _i32(add, cache.c.rows, "add"), _i32(refused_dev, 1, "refused_dev"), p, n,
+                                  _stream(stream)))
+
+
+def spt_cache_write(cache, layer, first, k, v, stream=None):
+    token, head = cache._tokens(k, "k", cache.c.heads)
+    if k.shape[0] != v.shape[0] or cache._tokens(v, "v", cache.c.heads) != (token, head):
+        _invalid("k and v must be alike")
+    _check(lib().spt_cache_write(_desc(cache), layer, _i32(first, cache.c.rows + 1, "first"), k.shape[0], _p(k), _p(v), token, head,
+                                 _stream(stream)))
+
+
+def spt_cache_compact(cache, first, keep, stream=None):
+    _check(lib().spt_cache_compact(_desc(cache), _i32(first, cache.c.rows + 1, "first"), keep and _desc(keep), _stream(stream)))
+
+
+def spt_cache_free(cache, new_len, stream=None):
+    _check(lib().spt_cache_free(_desc(cache), _i32(new_len, cache.c.rows, "new_len"), _stream(stream)))
+
+
+def spt_cache_fork(cache, parents, children, stream=None):
+    n = children.numel()
+    _check(lib().spt_cache_fork(_desc(cache), n, _i32(parents, n, "parents"), _i32(children, n, "children"), _stream(stream)))
+
+
+def spt_cache_attention(cache, layer, first, tree, q, scale, out, lse=None, ws=None, stream=None):
+    """q, out: (tokens, q_heads, width); tree: DeviceCSR or None; lse: float32 (tokens, q_heads), contiguous, or None."""
+    import torch
+    heads = q.shape[1] if q.dim() == 3 else 0
+    q_token, q_head = cache._tokens(q, "q", heads)
+    out_token, out_head = cache._tokens(out, "out", heads)
+    if out.shape[0] != q.shape[0]:
+        _invalid("q and out have different numbers of tokens")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous()):
+        _invalid("lse must be float32, (tokens, q_heads), contiguous")
+    p, n = _ws(ws)
+    _check(lib().spt_cache_attention(_desc(cache), layer, _i32(first, cache.c.rows + 1, "first"), q.shape[0], tree and _desc(tree),
+                                     _p(q), heads, q_token, q_head, scale, _p(out), out_token, out_head, _p(lse), p, n,
+                                     _stream(stream)))
+
+
+class LogitRules:
+    """spt_logit_rules of device tensors and DeviceCSR matrices; the number of sequences follows from first, else from what is
+    given for each sequence."""
+
+    def __init__(self, first=None, seen=None, tree=None, drafts=None, repetition=None, presence=None, frequency=None, bias=None,
+                 allowed=None, sequences=None):
+        import torch
+        per_sequence = [t for t in (repetition, presence, frequency) if t is not None]
+        if sequences is None:
+            counts = ([first.numel() - 1] if first is not None else []) + [m.c.level[0].N for m in (seen, bias) if m is not None]
+            counts += [t.numel() for t in per_sequence]
+            if not counts:
+                _invalid("the number of sequences is not given")
+            sequences = counts[0]
+        for t in per_sequence:
+            if t.dtype != torch.float32 or not t.is_contiguous() or t.numel() < sequences:
+                _invalid(f"repetition, presence and frequency must be contiguous float32 tensors of {sequences} entries")
+        if allowed is not None and (allowed.dtype not in (torch.int32, torch.uint32) or allowed.dim() != 2 or
+                                    _stride(allowed, 1) not in (0, 1)):
+            _invalid("allowed must be (rows, words) of 32 bits")
+        r = SptLogitRules()
+        r.first, r.sequences = _i32(first, sequences + 1, "first"), sequences
+        r.seen, r.tree, r.bias = (m and _desc(m) for m in (seen, tree, bias))
+        r.drafts = _i32(drafts, 0, "drafts")
+        r.repetition, r.presence, r.frequency = _p(repetition), _p(presence), _p(frequency)
+        if allowed is not None:
+            r.allowed, r.allowed_stride = allowed.data_ptr(), max(_stride(allowed, 0), allowed.shape[1])
+        self.keep = (first, seen, tree, drafts, repetition, presence, frequency, bias, allowed)
+        self.rows = min([t.shape[0] for t in (drafts, allowed) if t is not None], default=None)
+        self.c = r
+
+
+def spt_adjust_logits(logits, rules, out, stream=None):
+    """logits, out: (rows, vocabulary) of one dtype, values of a row contiguous; they may be the same tensor."""
+    if logits.dim() != 2 or logits.shape != out.shape or logits.dtype != out.dtype or _stride(logits, 1) > 1 or _stride(out, 1) > 1:
+        _invalid("logits and out must be alike: (rows, vocabulary), values of a row contiguous")
+    if rules.rows is not None and rules.rows < logits.shape[0]:
+        _invalid("drafts or allowed have fewer rows than logits")
+    R, V = logits.shape
+    stride, out_stride = (_stride(t, 0) if R > 1 else V for t in (logits, out))
+    _check(lib().spt_adjust_logits(_dtype_code(logits.dtype), R, V, _p(logits), stride, _desc(rules), _p(out), out_stride,
+                                   _stream(stream)))

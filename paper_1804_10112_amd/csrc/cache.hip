@@ -1,0 +1,347 @@
+// The pages of a cache: rows that are extended, written, compacted, cut and forked. All of it is integer work on the table and
+// copies of whole slots, so results do not depend on the order in which workgroups run.
+#include "cache.hpp"
+
+namespace spt {
+
+namespace {
+
+constexpr int kScanBlock = 1024;
+
+// Gives back the pages of row s at places from .. to-1. Called by a whole wave.
+__device__ __forceinline__ void release(const Cache& c, int s, int from, int to) {
+  for (int j = from + lane_id(); j < to; j += kWave) {
+    const int p = page_at(c, s, j);
+    if (p >= 0) atomicSub(&c.refs[p], 1);
+    c.table[static_cast<int64_t>(s) * c.row_pages + j] = -1;
+  }
+}
+
+// ---- free -------------------------------------------------------------------------------------------------------------------
+
+__global__ void free_kernel(Cache c, const int32_t* __restrict__ new_len) {
+  const int s = blockIdx.x * (kBlock / kWave) + wave_id();
+  if (s >= c.rows) return;
+  const int before = row_length(c, s), after = new_len[s];
+  if (after < 0 || after >= before) return;
+  release(c, s, pages_held(c, after), pages_held(c, before));
+  if (lane_id() == 0) c.len[s] = after;
+}
+
+// ---- fork -------------------------------------------------------------------------------------------------------------------
+
+// A workgroup for each entry. Parents are only read (an entry whose child is a parent is skipped) and each child belongs to one
+// entry, the last that names it, so entries do not meet; refs are atomic.
+__global__ void fork_kernel(Cache c, int n, const int32_t* __restrict__ parents, const int32_t* __restrict__ children) {
+  const int i = blockIdx.x, parent = parents[i], child = children[i];
+  if (parent < 0 || parent >= c.rows || child < 0 || child >= c.rows) return;
+  int barred = 0;
+  for (int k = threadIdx.x; k < n; k += blockDim.x) barred |= parents[k] == child || (k > i && children[k] == child);
+  if (__syncthreads_or(barred)) return;
+  const int length = row_length(c, parent), held = pages_held(c, length), old = pages_held(c, row_length(c, child));
+  __syncthreads();  // before the child's length changes
+  for (int j = threadIdx.x; j < (held > old ? held : old); j += blockDim.x) {
+    const int was = j < old ? page_at(c, child, j) : -1, is = j < held ? page_at(c, parent, j) : -1;
+    if (was >= 0) atomicSub(&c.refs[was], 1);
+    if (is >= 0) atomicAdd(&c.refs[is], 1);
+    c.table[static_cast<int64_t>(child) * c.row_pages + j] = is;
+  }
+  if (threadIdx.x == 0) c.len[child] = length;
+}
+
+// ---- extend -----------------------------------------------------------------------------------------------------------------
+//
+// Three launches. (1) Workgroups count the free pages of a stretch of the pool each; one more goes through the rows and writes
+// the running sum of the pages they want. (2) With both, the k-th free page finds the row and the place it goes to. (3) Copies
+// on write, lengths, and the shared pages' refs, which (1) and (2) both have to find as they were.
+
+struct Wanted {
+  int start, count;  // places start .. start+count-1 of the table
+  bool refused;
+};
+
+// What row s wants to hold `add` tokens more; copy: its last page is partly filled and shared.
+__device__ __forceinline__ Wanted wanted(const Cache& c, int length, int add, bool copy) {
+  if (add <= 0) return {0, 0, false};
+  if (add > (c.row_pages << c.shift) - length) return {0, 0, true};
+  const int start = pages_held(c, length) - copy;
+  return {start, pages_held(c, length + add) - start, false};
+}
+
+__device__ __forceinline__ int block_inclusive_scan(int v, int* lds) {
+  const int lane = lane_id(), wave = wave_id();
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const int o = __shfl_up(v, d);
+    if (lane >= d) v += o;
+  }
+  __syncthreads();
+  if (lane == kWave - 1) lds[wave] = v;
+  __syncthreads();
+  int before = 0;
+  for (int w = 0; w < wave; ++w) before += lds[w];
+  return v + before;
+}
+
+// What (1) leaves to (2) and (3), in the workspace.
+struct Plan {
+  int32_t* free_pages;  // of each stretch
+  int32_t* end;         // of each row: pages wanted by the rows up to it
+  int32_t* copied;      // of each row: its shared last page, or -1
+  int32_t* target;      // of each row: the page that takes its place
+  int32_t* fill;        // of each row: slots used of its last page, 0 = all
+  int32_t* total;       // free pages in all
+};
+
+__global__ void __launch_bounds__(kScanBlock) extend_count_kernel(Cache c, const int32_t* __restrict__ add, int stretch, Plan plan,
+                                                                  int32_t* refused) {
+  __shared__ int lds[kScanBlock / kWave];
+  if (blockIdx.x + 1 < gridDim.x) {
+    const int lo = blockIdx.x * stretch, hi = c.pages - lo < stretch ? c.pages : lo + stretch;
+    int n = 0;
+    for (int p = lo + threadIdx.x; p < hi; p += kScanBlock) n += c.refs[p] == 0;
+    n = block_inclusive_scan(n, lds);
+    if (threadIdx.x == kScanBlock - 1) plan.free_pages[blockIdx.x] = n;
+    return;
+  }
+  int before = 0;
+  for (int base = 0; base < c.rows; base += kScanBlock) {
+    const int s = base + threadIdx.x;
+    int n = 0, from = -1;
+    if (s < c.rows) {
+      const int length = row_length(c, s);
+      if (add[s] > 0 && (length & ((1 << c.shift) - 1)) != 0) {
+        const int p = page_at(c, s, length >> c.shift);
+        if (p >= 0 && c.refs[p] > 1) from = p;
+      }
+      n = wanted(c, length, add[s], from >= 0).count;
+      plan.copied[s] = from;
+      plan.fill[s] = length & ((1 << c.shift) - 1);
+    }
+    const int sum = before + block_inclusive_scan(n, lds);
+    if (s < c.rows) plan.end[s] = sum;
+    __syncthreads();
+    if (threadIdx.x == kScanBlock - 1) lds[0] = sum;
+    __syncthreads();
+    before = lds[0];
+  }
+  if (threadIdx.x == 0) *refused = 0;
+}
+
+__global__ void __launch_bounds__(kScanBlock) extend_assign_kernel(Cache c, const int32_t* __restrict__ add, int stretch, Plan plan) {
+  __shared__ int lds[kScanBlock / kWave];
+  __shared__ int sums[2];
+  if (threadIdx.x < 2) sums[threadIdx.x] = 0;
+  __syncthreads();
+  int mine = 0, all = 0;
+  for (int b = threadIdx.x; b < static_cast<int>(gridDim.x); b += kScanBlock) {
+    const int n = plan.free_pages[b];
+    all += n;
+    if (b < static_cast<int>(blockIdx.x)) mine += n;
+  }
+  if (mine) atomicAdd(&sums[0], mine);
+  if (all) atomicAdd(&sums[1], all);
+  __syncthreads();
+  int rank = sums[0];
+  const int total = sums[1];
+  if (blockIdx.x == 0 && threadIdx.x == 0) *plan.total = total;
+  const int needed = plan.end[c.rows - 1];
+  const int lo = blockIdx.x * stretch, hi = c.pages - lo < stretch ? c.pages : lo + stretch;
+  for (int base = lo; base < hi && rank < needed; base += kScanBlock) {
+    const int p = base + threadIdx.x;
+    const int is_free = p < hi && c.refs[p] == 0;
+    const int upto = rank + block_inclusive_scan(is_free, lds), k = upto - 1;
+    if (is_free && k < needed) {
+      int s = 0, n = c.rows;  // the first row with end > k
+      while (n > 0) {
+        const int half = n >> 1;
+        if (plan.end[s + half] <= k) s += half + 1, n -= half + 1;
+        else n = half;
+      }
+      if (plan.end[s] <= total) {
+        const Wanted w = wanted(c, row_length(c, s), add[s], plan.copied[s] >= 0);
+        const int place = k - (plan.end[s] - w.count);
+        c.table[static_cast<int64_t>(s) * c.row_pages + w.start + place] = p;
+        c.refs[p] = 1;
+        if (place == 0) plan.target[s] = p;
+      }
+    }
+    __syncthreads();
+    if (threadIdx.x == kScanBlock - 1) lds[0] = upto;
+    __syncthreads();
+    rank = lds[0];
+    __syncthreads();
+  }
+}
+
+// Rows by blockIdx.x; the slots to copy are dealt out over blockIdx.y, the last of which does the row's numbers.
+__global__ void extend_finish_kernel(Cache c, const int32_t* __restrict__ add, Plan plan, int32_t* refused) {
+  const int s = blockIdx.x, from = plan.copied[s], fill = plan.fill[s];
+  const int wants = plan.end[s] - (s ? plan.end[s - 1] : 0);
+  const bool served = wants == 0 || plan.end[s] <= *plan.total;
+  if (blockIdx.y + 1 == gridDim.y) {
+    if (threadIdx.x != 0) return;
+    const int length = row_length(c, s);
+    if (!served || wanted(c, length, add[s], from >= 0).refused) {
+      atomicAdd(refused, 1);
+    } else if (add[s] > 0) {
+      c.len[s] = length + add[s];
+      if (wants && from >= 0) atomicSub(&c.refs[from], 1);
+    }
+    return;
+  }
+  if (from < 0 || wants == 0 || !served) return;
+  const int to = plan.target[s], vecs = c.width_bytes / 16;
+  const int64_t units = static_cast<int64_t>(c.layers) * fill * c.heads * vecs * 2;
+  for (int64_t u = blockIdx.y * static_cast<int64_t>(blockDim.x) + threadIdx.x; u < units;
+       u += static_cast<int64_t>(gridDim.y - 1) * blockDim.x) {
+    int64_t r = u;
+    const int v = r % vecs;
+    r /= vecs;
+    const int h = r % c.heads;
+    r /= c.heads;
+    const int o = r % fill;
+    r /= fill;
+    char* pool = (r & 1) ? c.V : c.K;
+    pool += (r >> 1) * c.layer_bytes + o * c.slot_bytes + h * c.head_bytes + v * 16;
+    *reinterpret_cast<int4*>(pool + to * c.page_bytes) = *reinterpret_cast<const int4*>(pool + from * c.page_bytes);
+  }
+}
+
+// ---- write ------------------------------------------------------------------------------------------------------------------
+
+// A wave for each token.
+__global__ void write_kernel(Cache c, int layer, const int32_t* __restrict__ first, int total, const char* __restrict__ k,
+                             const char* __restrict__ v, int64_t token_bytes, int64_t in_head_bytes) {
+  const int i = blockIdx.x * (kBlock / kWave) + wave_id();
+  if (i >= total) return;
+  const int s = wave_row_of(first, c.rows, i);
+  if (s < 0) return;
+  const Drafted d = drafted(first, s, total);
+  const int length = row_length(c, s), t = length - d.count + i - d.begin;
+  if (t < 0 || t >= length) return;
+  const int page = page_at(c, s, t >> c.shift);
+  if (page < 0) return;
+  const int64_t at = layer * c.layer_bytes + page * c.page_bytes + (t & ((1 << c.shift) - 1)) * c.slot_bytes;
+  const int vecs = c.width_bytes / 16;
+  for (int u = lane_id(); u < c.heads * vecs; u += kWave) {
+    const int h = u / vecs, e = (u - h * vecs) * 16;
+    const int64_t from = i * token_bytes + h * in_head_bytes + e, to = at + h * c.head_bytes + e;
+    *reinterpret_cast<int4*>(c.K + to) = *reinterpret_cast<const int4*>(k + from);
+    *reinterpret_cast<int4*>(c.V + to) = *reinterpret_cast<const int4*>(v + from);
+  }
+}
+
+// ---- compact ----------------------------------------------------------------------------------------------------------------
+
+// Drafted tokens that a row has and keeps.
+__device__ __forceinline__ int kept(const Cache& c, const Pattern& keep, int s, int drafts) {
+  return clamped(pattern_end(keep, s) - pattern_begin(keep, s), 0, drafts);
+}
+
+// A thread owns 16 bytes of each token of the row (in one layer, K or V, and head) and moves them token after token: the kept ones
+// ascend, so a slot that is written was read before and is not read again.
+__global__ void compact_move_kernel(Cache c, const int32_t* __restrict__ first, Pattern keep) {
+  const int s = blockIdx.x, vecs = c.width_bytes / 16;
+  int64_t r = blockIdx.y * static_cast<int64_t>(blockDim.x) + threadIdx.x;
+  if (r >= static_cast<int64_t>(c.layers) * 2 * c.heads * vecs) return;
+  const int v = r % vecs;
+  r /= vecs;
+  const int h = r % c.heads;
+  r /= c.heads;
+  char* pool = ((r & 1) ? c.V : c.K) + (r >> 1) * c.layer_bytes + h * c.head_bytes + v * 16;
+  const Drafted d = drafted(first, s, INT32_MAX);
+  const int context = row_length(c, s) - d.count, begin = pattern_begin(keep, s), n = kept(c, keep, s, d.count);
+  if (context < 0) return;
+  for (int j = 0; j < n; ++j) {
+    const int from = keep.crd[begin + j];
+    if (from <= j || from >= d.count) continue;
+    const int a = context + from, b = context + j, pa = page_at(c, s, a >> c.shift), pb = page_at(c, s, b >> c.shift);
+    if (pa < 0 || pb < 0) continue;
+    const int mask = (1 << c.shift) - 1;
+    *reinterpret_cast<int4*>(pool + pb * c.page_bytes + (b & mask) * c.slot_bytes) =
+        *reinterpret_cast<const int4*>(pool + pa * c.page_bytes + (a & mask) * c.slot_bytes);
+  }
+}
+
+__global__ void compact_cut_kernel(Cache c, const int32_t* __restrict__ first, Pattern keep) {
+  const int s = blockIdx.x * (kBlock / kWave) + wave_id();
+  if (s >= c.rows) return;
+  const Drafted d = drafted(first, s, INT32_MAX);
+  const int before = row_length(c, s), context = before - d.count;
+  if (context < 0 || d.count == 0) return;
+  const int after = context + kept(c, keep, s, d.count);
+  release(c, s, pages_held(c, after), pages_held(c, before));
+  if (lane_id() == 0) c.len[s] = after;
+}
+
+int stretch_of(int64_t pages) {
+  const int64_t s = (pages + 1023) / 1024;
+  return s < kScanBlock ? kScanBlock : static_cast<int>(s);
+}
+
+}  // namespace
+
+size_t cache_extend_workspace(const spt_cache* c) {
+  return 4 * align_up(static_cast<size_t>(c->rows) * 4, 256) + align_up(1024 * 4, 256) + 256;
+}
+
+spt_status cache_extend_dispatch(const spt_cache* cache, const int32_t* add, int32_t* refused, void* ws, hipStream_t stream) {
+  const Cache c = cache_view(cache);
+  Workspace w(ws, cache_extend_workspace(cache));
+  Plan plan;
+  plan.free_pages = w.take<int32_t>(1024);
+  plan.end = w.take<int32_t>(c.rows);
+  plan.copied = w.take<int32_t>(c.rows);
+  plan.target = w.take<int32_t>(c.rows);
+  plan.fill = w.take<int32_t>(c.rows);
+  plan.total = w.take<int32_t>(1);
+  const int stretch = stretch_of(c.pages), blocks = c.pages ? (c.pages + stretch - 1) / stretch : 1;
+  extend_count_kernel<<<blocks + 1, kScanBlock, 0, stream>>>(c, add, stretch, plan, refused);
+  if (c.rows == 0) {
+    SPT_CHECK_LAUNCH("cache_extend");
+    return SPT_OK;
+  }
+  extend_assign_kernel<<<blocks, kScanBlock, 0, stream>>>(c, add, stretch, plan);
+  const int64_t units = static_cast<int64_t>(c.layers) * 2 * c.heads * (c.width_bytes / 16) << c.shift;
+  int64_t y = (units + 8 * kBlock - 1) / (8 * kBlock);
+  const int64_t most = c.rows < 8192 ? 8192 / c.rows : 1;
+  y = y > most ? most : y;
+  extend_finish_kernel<<<dim3(c.rows, static_cast<unsigned>(y) + 1), kBlock, 0, stream>>>(c, add, plan, refused);
+  SPT_CHECK_LAUNCH("cache_extend");
+  return SPT_OK;
+}
+
+spt_status cache_free_dispatch(const spt_cache* cache, const int32_t* new_len, hipStream_t stream) {
+  const Cache c = cache_view(cache);
+  free_kernel<<<(c.rows + 3) / 4, kBlock, 0, stream>>>(c, new_len);
+  SPT_CHECK_LAUNCH("cache_free");
+  return SPT_OK;
+}
+
+spt_status cache_fork_dispatch(const spt_cache* cache, int n, const int32_t* parents, const int32_t* children, hipStream_t stream) {
+  fork_kernel<<<n, kBlock, 0, stream>>>(cache_view(cache), n, parents, children);
+  SPT_CHECK_LAUNCH("cache_fork");
+  return SPT_OK;
+}
+
+spt_status cache_write_dispatch(const spt_cache* cache, int layer, const int32_t* first, int total, const void* k, const void* v,
+                                int64_t token_stride, int64_t head_stride, hipStream_t stream) {
+  const int64_t b = value_bytes(cache->dtype);
+  write_kernel<<<(total + 3) / 4, kBlock, 0, stream>>>(cache_view(cache), layer, first, total, static_cast<const char*>(k),
+                                                       static_cast<const char*>(v), token_stride * b, head_stride * b);
+  SPT_CHECK_LAUNCH("cache_write");
+  return SPT_OK;
+}
+
+spt_status cache_compact_dispatch(const spt_cache* cache, const int32_t* first, const spt_tensor* keep, hipStream_t stream) {
+  const Cache c = cache_view(cache);
+  const Pattern k = pattern_view(keep);
+  const int64_t threads = static_cast<int64_t>(c.layers) * 2 * c.heads * (c.width_bytes / 16);
+  compact_move_kernel<<<dim3(c.rows, static_cast<unsigned>((threads + kBlock - 1) / kBlock)), kBlock, 0, stream>>>(c, first, k);
+  compact_cut_kernel<<<(c.rows + 3) / 4, kBlock, 0, stream>>>(c, first, k);
+  SPT_CHECK_LAUNCH("cache_compact");
+  return SPT_OK;
+}
+
+}  // namespace spt
