@@ -1,0 +1,378 @@
+// Attention of drafted tokens over the pages of a cache: what its kernels share.
+//
+// A tile is up to 16, 32, 64 or 128 rows (drafted token, query head) of one sequence that share a head of K and V; rows run token by token, the
+// heads of a group side by side. A tile goes through its tokens in steps, once, with the running maximum m and sum l of the softmax:
+//   z = scale log2(e) K Q^T,  m' = max(m, z),  P = exp2(z - m'),  l = l exp2(m - m') + sum P,  O^T = O^T exp2(m - m') + V^T P.
+// Both products are matrix instructions of 16 x 16 with the tokens as rows of the first result and as the inner dimension of the
+// second: a lane then holds, for one row, the tokens 4q .. 4q+3 of each 16 (q = lane / 16), and since the order of an inner dimension
+// is free, its P is the operand of the second product as it stands. V is turned round on its way out of LDS.
+//
+// The work of a call is all steps of all tiles, a number that only the device knows (lengths change between calls of one captured
+// graph). Each workgroup of a fixed grid finds its equal share of it from len and first: a range of steps that may begin and end
+// within a tile. A tile that lies in one workgroup goes to `out` at once; one that does not leaves m, l and O of each part in the
+// workspace, at most two parts a workgroup, and a second kernel joins them.
+#pragma once
+#include "cache.hpp"
+#include "values.hpp"
+
+namespace spt {
+
+constexpr int kWaves = kBlock / kWave;
+// Workgroups of the grid, as many as run at once on 256 compute units: two each, one where a lane has to hold more than 256 registers.
+constexpr int kMostGroups = 512;
+template <int ROW_BYTES, int SIZE>
+constexpr int groups_of() {
+  return ROW_BYTES > (SIZE == 4 ? 512 : 256) ? 256 : 512;
+}
+
+typedef int i4 __attribute__((ext_vector_type(4)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+using LdsQuad = __attribute__((address_space(3))) s4;
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+
+// Which part of the call a workgroup began within a tile, for the joining kernel.
+struct Part {
+  int parts;  // of the tile, if this workgroup's is the second of them; else 0
+  int s, head, row;
+};
+
+struct Attention {
+  Cache c;
+  int layer, total, q_heads, group;
+  const int32_t* first;
+  Pattern tree;  // pos NULL: each token sees those up to itself
+  const char* q;
+  char* out;
+  float* lse;
+  int64_t q_token_bytes, q_head_bytes, out_token_bytes, out_head_bytes;
+  float scale;  // times log2(e)
+  Part* part;   // of each workgroup
+  float* partial;  // two slots for each workgroup: m[rows], l[rows], O[rows][width]
+};
+
+template <class T>
+__device__ __forceinline__ f4 multiply(i4 a, i4 b, f4 c);  // c += a (16 x 64 bytes of values) times b
+template <>
+__device__ __forceinline__ f4 multiply<bf16>(i4 a, i4 b, f4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+}
+template <>
+__device__ __forceinline__ f4 multiply<f16>(i4 a, i4 b, f4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+}
+template <>
+__device__ __forceinline__ f4 multiply<float>(i4 a, i4 b, f4 c) {
+  const f4 x = __builtin_bit_cast(f4, a), y = __builtin_bit_cast(f4, b);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], c, 0, 0, 0);
+  return c;
+}
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
+
+// Whether one of the values in 16 bytes is an infinity or a NaN.
+template <class T>
+__device__ __forceinline__ bool any_not_finite(i4 v) {
+  bool bad = false;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t x = v[e];
+    if (sizeof(T) == 4) {
+      bad |= (x & 0x7f800000u) == 0x7f800000u;
+    } else {
+      const uint32_t ones = sizeof(T) == 2 && __is_same(T, f16) ? 0x7c00u : 0x7f80u;
+      bad |= (x & ones) == ones || (x >> 16 & ones) == ones;
+    }
+  }
+  return bad;
+}
+
+// Tiles of ROWS rows that go through their tokens STEP at a time.
+template <int ROWS, int STEP>
+struct Plan {
+  static constexpr int kRows = ROWS;
+  const Attention& a;
+
+  struct Sequence {
+    Drafted d;
+    int length, context, rows, tiles;  // context: tokens before the drafted ones, below 0 where some of those are not there
+  };
+  __device__ __forceinline__ Sequence sequence(int s) const {
+    Sequence q;
+    q.d = drafted(a.first, s, a.total);
+    q.length = a.c.pages ? row_length(a.c, s) : 0;
+    q.context = q.length - q.d.count;
+    q.rows = q.d.count * a.group;
+    q.tiles = (q.rows + ROWS - 1) / ROWS;
+    return q;
+  }
+  // Tokens that the rows of a tile can see.
+  __device__ __forceinline__ int end(const Sequence& q, int tile) const {
+    if (a.tree.pos) return q.length;
+    const int last = (tile + 1) * ROWS < q.rows ? (tile + 1) * ROWS - 1 : q.rows - 1;
+    const int e = q.context + last / a.group + 1;
+    return e > 0 ? e : 0;
+  }
+  __device__ __forceinline__ int steps(const Sequence& q, int tile) const {
+    const int e = end(q, tile);
+    return e > 0 ? (e + STEP - 1) / STEP : 1;  // one for a tile that sees nothing, whose rows have to be written
+  }
+  __device__ __forceinline__ int64_t head_steps(const Sequence& q) const {
+    if (q.tiles == 0) return 0;
+    if (a.tree.pos || q.tiles == 1) return static_cast<int64_t>(q.tiles) * steps(q, q.tiles - 1);
+    int64_t n = 0;
+    for (int t = 0; t < q.tiles; ++t) n += steps(q, t);
+    return n;
+  }
+};
+
+__device__ __forceinline__ int64_t block_inclusive_scan(int64_t v, int64_t* lds) {
+  const int lane = lane_id(), wave = wave_id();
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const int64_t o = __shfl_up(static_cast<long long>(v), d);
+    if (lane >= d) v += o;
+  }
+  __syncthreads();
+  if (lane == kWave - 1) lds[wave] = v;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) v += lds[w];
+  return v;
+}
+
+// Finds the sequence that the workgroup's share begins in: `begin` becomes the steps before it within the sequence. All threads of
+// the workgroup; false if the share is empty.
+template <class P>
+__device__ __forceinline__ bool share(const P& plan, int group, int groups, int64_t* lds, int64_t* found, int64_t& per, int64_t& begin, int64_t& end,
+                                      int& s) {
+  const int rows = plan.a.c.rows, heads = plan.a.c.heads;
+  int64_t total = 0, mine = 0, upto = 0;
+  for (int base = 0; base < rows; base += kBlock) {
+    const int r = base + threadIdx.x;
+    mine = r < rows ? plan.head_steps(plan.sequence(r)) * heads : 0;
+    upto = total + block_inclusive_scan(mine, lds);
+    __syncthreads();
+    if (threadIdx.x == kBlock - 1) lds[0] = upto;
+    __syncthreads();
+    total = lds[0];
+    __syncthreads();
+  }
+  per = (total + groups - 1) / groups;
+  begin = group * per;
+  end = begin + per < total ? begin + per : total;
+  if (begin >= end) return false;
+  int64_t before = 0;
+  for (int base = 0; base < rows; base += kBlock) {
+    const int r = base + threadIdx.x;
+    if (rows > kBlock) {
+      mine = r < rows ? plan.head_steps(plan.sequence(r)) * heads : 0;
+      upto = before + block_inclusive_scan(mine, lds);
+    }
+    if (upto > begin && upto - mine <= begin) found[0] = r, found[1] = upto - mine;
+    __syncthreads();
+    if (threadIdx.x == kBlock - 1) lds[0] = upto;
+    __syncthreads();
+    before = lds[0];
+    __syncthreads();
+    if (before > begin) break;
+  }
+  s = __builtin_amdgcn_readfirstlane(static_cast<int>(found[0]));
+  const int64_t skipped = found[1];
+  begin -= skipped;
+  end -= skipped;
+  return true;
+}
+
+// A workgroup's way through its share: tile by tile, the steps [step, stop) of each.
+template <class P>
+struct Walk {
+  P plan;
+  typename P::Sequence q;
+  int s, head, tile, step, steps, stop;
+  int64_t left;
+
+  // False if the share is empty. Notes in `part` whether the workgroup begins with a tile's second part.
+  __device__ __forceinline__ bool start(int group, int groups, int64_t* lds, int64_t* found) {
+    int64_t per = 0, at = 0, end = 0;
+    const bool some = share(plan, group, groups, lds, found, per, at, end, s);
+    Part part{0, 0, 0, 0};
+    if (some) {  // `at` counts the steps of sequence s, head by head and tile by tile
+      q = plan.sequence(s);
+      const int64_t in_head = plan.head_steps(q);
+      head = static_cast<int>(at / in_head);
+      tile = 0;
+      int64_t rest = at - head * in_head;
+      steps = plan.steps(q, 0);
+      while (rest >= steps) rest -= steps, steps = plan.steps(q, ++tile);
+      step = static_cast<int>(rest);
+      left = end - at;
+      limit();
+      if (step > 0 && step <= per) part = {static_cast<int>(1 + (steps - step + per - 1) / per), s, head, tile * P::kRows};
+    }
+    if (threadIdx.x == 0) plan.a.part[group] = part;
+    return some;
+  }
+  __device__ __forceinline__ void limit() { stop = steps - step <= left ? steps : step + static_cast<int>(left); }
+  __device__ __forceinline__ bool next() {
+    left -= stop - step;
+    if (left == 0) return false;
+    step = 0;
+    if (++tile == q.tiles) {
+      tile = 0;
+      if (++head == plan.a.c.heads) {
+        head = 0;
+        do q = plan.sequence(++s);
+        while (q.tiles == 0);
+      }
+    }
+    steps = plan.steps(q, tile);
+    limit();
+    return true;
+  }
+};
+
+// Rows row0 + 16 n + i of a tile: 16 bytes of a lane from each 64 of the head, zeros behind the rows and the width.
+template <int NQ, int CHUNKS, class Q>
+__device__ __forceinline__ void load_queries(const Attention& a, const Q& q, int head, int row0, i4 (&x)[NQ][CHUNKS]) {
+  const int i = lane_id() & 15, quad = lane_id() >> 4, vecs = a.c.width_bytes / 16;
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const int row = row0 + 16 * n + i, token = row / a.group;
+    const char* from = a.q + (q.d.begin + token) * a.q_token_bytes + (head * a.group + row - token * a.group) * a.q_head_bytes;
+#pragma unroll
+    for (int j = 0; j < CHUNKS; ++j) {
+      x[n][j] = i4{0, 0, 0, 0};
+      if (row < q.rows && quad + 4 * j < vecs) x[n][j] = *reinterpret_cast<const i4*>(from + (quad + 4 * j) * 16);
+    }
+  }
+}
+
+// Which of the 32 tokens from `base` on a row sees, as bits; the four lanes of a row share the work and get the same.
+template <class Q>
+__device__ __forceinline__ uint32_t row_sight(const Attention& a, const Q& q, int row, int base) {
+  const int quad = lane_id() >> 4, token = row / a.group;
+  uint32_t bits = low_bits(q.context - base);
+  if (row >= q.rows) {
+    bits = 0;
+  } else if (!a.tree.pos) {
+    bits = low_bits(q.context + token + 1 - base);
+  } else if (base + 32 > q.context) {
+    const int r = q.d.begin + token, end = pattern_end(a.tree, r);
+    for (int e = pattern_begin(a.tree, r) + quad; e < end; e += 4) {
+      const int j = a.tree.crd[e];
+      if (j >= 0 && j < q.d.count) {
+        const int b = q.context + j - base;
+        if (b >= 0 && b < 32) bits |= 1u << b;
+      }
+    }
+  }
+  bits |= __shfl_xor(bits, 16);
+  bits |= __shfl_xor(bits, 32);
+  return bits;
+}
+
+// 16 bytes `chunk` of a token of K or V lie where reads of four tokens by 16 lanes, reads of eight tokens by eight lanes and writes
+// alike meet all banks.
+template <int ROW_BYTES>
+__device__ __forceinline__ int swizzled(int token, int chunk) {
+  const int turn = ROW_BYTES % 256 == 0 ? (token & 7) << 1 : (token >> 1 & 3) << 1;
+  return token * ROW_BYTES + (chunk ^ turn) * 16;
+}
+
+// V^T of 16 values of the head and 64 bytes' worth of tokens (32, or 16 of float32), out of LDS.
+template <class T, int ROW_BYTES>
+__device__ __forceinline__ i4 turned_values(char* area, int token, int d) {
+  const int i = lane_id() & 15, quad = lane_id() >> 4;
+  if constexpr (sizeof(T) == 4) {
+    i4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const int*>(area + swizzled<ROW_BYTES>(token + 4 * quad + e, 4 * d + (i >> 2)) + (i & 3) * 4);
+    return v;
+  } else {
+    s4 half[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      half[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (LdsQuad*)(area + swizzled<ROW_BYTES>(token + 16 * u + 4 * quad + (i >> 2), 2 * d + (i >> 1 & 1)) + (i & 1) * 8));
+    return __builtin_bit_cast(i4, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+}
+
+// One step of the softmax of 16 rows: scores z (16 tokens each, 4q .. 4q+3 of a lane) become weights. seen: bits of 32 tokens each, read
+// where not all are seen.
+template <int SUB, int TILES>
+__device__ __forceinline__ void softmax_step(f4 (&z)[SUB], float scale, bool all, const uint32_t* seen, float& m, float& l, f4 (&o)[TILES]) {
+  const int quad = lane_id() >> 4;
+  float top = m;
+#pragma unroll
+  for (int u = 0; u < SUB; ++u)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      z[u][r] *= scale;
+      if (!all && !(seen[u / 2] >> (16 * (u & 1) + 4 * quad + r) & 1)) z[u][r] = -INFINITY;
+      top = fmaxf(top, z[u][r]);
+    }
+  top = fmaxf(top, __shfl_xor(top, 16));
+  top = fmaxf(top, __shfl_xor(top, 32));
+  const float zero = top == -INFINITY ? 0 : top;
+  if (__any(top != m)) {
+    const float keep = exp2_of(m - zero);
+    l *= keep;
+#pragma unroll
+    for (int d = 0; d < TILES; ++d) o[d] *= keep;
+    m = top;
+  }
+#pragma unroll
+  for (int u = 0; u < SUB; ++u)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      z[u][r] = exp2_of(z[u][r] - zero);
+      l += z[u][r];
+    }
+}
+
+// The weights of 32 tokens (16 of float32) as an operand. They are rounded to the values' type, which the matrix instruction takes:
+// half a step of it (2^-9 of a weight in bf16, 2^-12 in f16), no more than the rounding of the result; their sum l is not rounded.
+template <class T>
+__device__ __forceinline__ i4 weights(const f4* z) {
+  if constexpr (sizeof(T) == 4) {
+    return __builtin_bit_cast(i4, z[0]);
+  } else {
+    typedef T t8 __attribute__((ext_vector_type(8)));
+    t8 w;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = from_float<T>(z[e >> 2][e & 3]);
+    return __builtin_bit_cast(i4, w);
+  }
+}
+
+// What a matrix instruction cannot do: a value of V that is not finite is to reach the rows that see its token and no others. Such tokens
+// are zeros in LDS; here their values are added one by one. w: the weight of the lane's row.
+template <class T, int TILES>
+__device__ __forceinline__ void add_token(const char* value, int width, bool seen, float w, f4 (&o)[TILES]) {
+  const int quad = lane_id() >> 4;
+#pragma unroll
+  for (int d = 0; d < TILES; ++d)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int e = 16 * d + 4 * quad + r;
+      if (e < width && seen) o[d][r] += w * to_float(reinterpret_cast<const T*>(value)[e]);
+    }
+}
+
+__device__ __forceinline__ float natural_lse(float m, float l) {
+  return l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+// The kernel for many rows (its own translation unit).
+template <class T>
+void launch_many_rows(const Attention& a, bool most, hipStream_t stream);
+// Joins the parts that kernels with tiles of `rows` rows and heads padded to `width` values left.
+template <class T>
+void launch_join(const Attention& a, int groups, int rows, int width, hipStream_t stream);
+
+}  // namespace spt

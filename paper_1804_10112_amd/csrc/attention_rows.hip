@@ -1,0 +1,227 @@
+// Attention of drafted tokens over the pages of a cache: the kernel for many rows.
+//
+// The four waves of a workgroup take 16 NQ rows each and the same tokens, 64 a step: K and V come to LDS once for all of them, two
+// steps' worth of it, so that the loads of one step (in registers) are under way while the other is multiplied.
+#include "attention.hpp"
+
+namespace spt {
+
+namespace {
+
+constexpr int kStep = 64;
+
+template <class T, int ROW_BYTES, int NQ, bool FULL>
+__global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 256)) attention_rows_kernel(Attention a) {
+  constexpr int kChunks = ROW_BYTES / 64, kWidth = ROW_BYTES / sizeof(T), kTiles = kWidth / 16, kVecs = ROW_BYTES / 16;
+  constexpr int kRows = 16 * NQ * kWaves, kGroups = groups_of<ROW_BYTES, sizeof(T)>(), kSub = kStep / 16;
+  constexpr int kLoads = kStep * kVecs / kBlock, kTokensApart = kBlock / kVecs;  // of a thread: 16 bytes of tokens so far apart
+  using P = Plan<kRows, kStep>;
+  __shared__ __attribute__((aligned(16))) char area[2][2][kStep * ROW_BYTES];  // K and V of two steps
+  __shared__ int64_t sums[kWaves], found[2];
+  __shared__ uint32_t absent[3][2], bad[3][2];  // bits of the tokens of a step that are not there, that hold values not finite
+  const Cache& c = a.c;
+  const int group = xcd_contiguous_block_id(), lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), i = lane & 15,
+            quad = lane >> 4, vecs = c.width_bytes / 16, width = c.width_bytes / sizeof(T);
+  const int chunk = threadIdx.x % kVecs, token0 = threadIdx.x / kVecs, chunk_read = FULL || chunk < vecs ? chunk : vecs - 1;
+  Walk<P> at{{a}};
+  if (!at.start(group, kGroups, sums, found)) return;
+
+  do {
+    const int row0 = at.tile * kRows + wave * 16 * NQ, tokens = at.plan.end(at.q, at.tile);
+    // tokens that some row of the wave can see: 0 for a wave behind the rows
+    const int last = row0 + 16 * NQ < at.q.rows ? row0 + 16 * NQ - 1 : at.q.rows - 1;
+    const int seen_end = row0 >= at.q.rows ? 0 : a.tree.pos ? tokens : at.q.context + last / a.group + 1;
+    i4 qf[NQ][kChunks];
+    load_queries(a, at.q, at.head, row0, qf);
+    f4 o[NQ][kTiles];
+    float m[NQ], l[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      m[n] = -INFINITY;
+      l[n] = 0;
+#pragma unroll
+      for (int d = 0; d < kTiles; ++d) o[n][d] = f4{0, 0, 0, 0};
+    }
+
+    const int64_t pool = a.layer * c.layer_bytes + at.head * c.head_bytes;
+    int page[kLoads], page_ahead[kLoads];
+    i4 k[kLoads], v[kLoads];
+    auto pages = [&](int base, int(&p)[kLoads]) {
+#pragma unroll
+      for (int x = 0; x < kLoads; ++x) {
+        const int t = base + token0 + x * kTokensApart;
+        p[x] = t < tokens ? page_at(c, at.s, t >> c.shift) : -1;
+      }
+    };
+    // As in the kernel for few rows: the pool's first slot for tokens that are nowhere.
+    auto load = [&](int base) {
+#pragma unroll
+      for (int x = 0; x < kLoads; ++x) {
+        const int t = base + token0 + x * kTokensApart;
+        const int64_t place =
+            pool + (page[x] < 0 ? 0 : page[x] * c.page_bytes + (t & ((1 << c.shift) - 1)) * c.slot_bytes) + chunk_read * 16;
+        k[x] = *reinterpret_cast<const i4*>(c.K + place);
+        v[x] = *reinterpret_cast<const i4*>(c.V + place);
+      }
+    };
+    // To LDS, with what the step's flags have to say of these tokens.
+    auto store = [&](int base, int buffer, int flag) {
+#pragma unroll
+      for (int x = 0; x < kLoads; ++x) {
+        const int t = token0 + x * kTokensApart;
+        if (page[x] < 0) {
+          if (chunk == 0) atomicOr(&absent[flag][t >> 5], 1u << (t & 31));
+          v[x] = i4{0, 0, 0, 0};
+        } else if (base + kStep > at.q.context && any_not_finite<T>(v[x])) {
+          atomicOr(&bad[flag][t >> 5], 1u << (t & 31));
+        }
+        if (!FULL && chunk >= vecs) k[x] = i4{0, 0, 0, 0};
+        *reinterpret_cast<i4*>(area[0][buffer] + swizzled<ROW_BYTES>(t, chunk)) = k[x];
+        *reinterpret_cast<i4*>(area[1][buffer] + swizzled<ROW_BYTES>(t, chunk)) = v[x];
+      }
+    };
+
+    if (threadIdx.x < 6) (&absent[0][0])[threadIdx.x] = 0, (&bad[0][0])[threadIdx.x] = 0;
+    const int base0 = at.step * kStep, limit = tokens > 0 ? at.stop * kStep : base0;
+    if (base0 < limit) {
+      pages(base0, page);
+      load(base0);
+      pages(base0 + kStep, page_ahead);
+      __syncthreads();
+      store(base0, 0, 0);
+#pragma unroll
+      for (int x = 0; x < kLoads; ++x) page[x] = page_ahead[x];
+      load(base0 + kStep);
+      pages(base0 + 2 * kStep, page_ahead);
+      lds_barrier();
+    }
+    int flag = 0, buffer = 0;
+    for (int base = base0; base < limit; base += kStep) {
+      const int next_flag = flag == 2 ? 0 : flag + 1, free_flag = next_flag == 2 ? 0 : next_flag + 1;
+      const uint32_t gone[2] = {absent[flag][0], absent[flag][1]};
+      uint32_t odd[2] = {bad[flag][0], bad[flag][1]};
+      if (threadIdx.x < 2) absent[free_flag][threadIdx.x] = 0, bad[free_flag][threadIdx.x] = 0;  // read a step ago, written to in the next
+      if (odd[0] | odd[1]) {
+        for (int x = threadIdx.x; x < kStep * kVecs; x += kBlock)
+          if (odd[x / kVecs >> 5] >> (x / kVecs & 31) & 1)
+            *reinterpret_cast<i4*>(area[1][buffer] + swizzled<ROW_BYTES>(x / kVecs, x % kVecs)) = i4{0, 0, 0, 0};
+        lds_barrier();
+      }
+      const bool work = base < seen_end;
+      f4 z[NQ][kSub];
+      if (work)
+#pragma unroll
+        for (int u = 0; u < kSub; ++u) {
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) z[n][u] = f4{0, 0, 0, 0};
+#pragma unroll
+          for (int j = 0; j < kChunks; ++j) {
+            const i4 kf = *reinterpret_cast<const i4*>(area[0][buffer] + swizzled<ROW_BYTES>(16 * u + i, quad + 4 * j));
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) z[n][u] = multiply<T>(kf, qf[n][j], z[n][u]);
+          }
+        }
+      if (base + kStep < limit) {
+        store(base + kStep, buffer ^ 1, next_flag);
+#pragma unroll
+        for (int x = 0; x < kLoads; ++x) page[x] = page_ahead[x];
+        load(base + 2 * kStep);
+        pages(base + 3 * kStep, page_ahead);
+      }
+      if (work) {
+        const bool all = base + kStep <= at.q.context && (gone[0] | gone[1]) == 0;
+        uint32_t sight[NQ][2];
+        if (!all)
+#pragma unroll
+          for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) sight[n][w] = row_sight(a, at.q, row0 + 16 * n + i, base + 32 * w) & ~gone[w];
+        i4 p[NQ][kSub / 2];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          softmax_step(z[n], a.scale, all, sight[n], m[n], l[n], o[n]);
+#pragma unroll
+          for (int w = 0; w < kSub / 2; ++w) p[n][w] = weights<T>(&z[n][2 * w]);
+        }
+#pragma unroll
+        for (int d = 0; d < kTiles; ++d)
+#pragma unroll
+          for (int w = 0; w < kSub / 2; ++w) {
+            const i4 vf = turned_values<T, ROW_BYTES>(area[1][buffer], 32 * w, d);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) o[n][d] = multiply<T>(vf, p[n][w], o[n][d]);
+          }
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+          while (odd[w]) {
+            const int b = __builtin_ctz(odd[w]), t = base + 32 * w + b, where = page_at(c, at.s, t >> c.shift);
+            odd[w] &= odd[w] - 1;
+            if (where < 0) continue;
+            const char* value = c.V + pool + where * c.page_bytes + (t & ((1 << c.shift) - 1)) * c.slot_bytes;
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+              float weight = 0;
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if ((b >> 4) * 4 + (b & 3) == e) weight = __shfl(z[n][2 * w + (e >> 2)][e & 3], (b & 12) * 4 + i);
+              add_token<T>(value, width, sight[n][w] >> b & 1, weight, o[n]);
+            }
+          }
+      }
+      lds_barrier();
+      flag = next_flag;
+      buffer ^= 1;
+    }
+
+    const bool whole = at.step == 0 && at.stop == at.steps;
+    float* slot = a.partial + static_cast<int64_t>(2 * group + (at.step == 0)) * kRows * (kWidth + 2);
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      l[n] += __shfl_xor(l[n], 16);
+      l[n] += __shfl_xor(l[n], 32);
+      const int in_tile = wave * 16 * NQ + 16 * n + i, row = row0 + 16 * n + i;
+      if (row >= at.q.rows) continue;
+      if (!whole) {
+#pragma unroll
+        for (int d = 0; d < kTiles; ++d)
+          *reinterpret_cast<f4*>(slot + 2 * kRows + static_cast<int64_t>(in_tile) * kWidth + 16 * d + 4 * quad) = o[n][d];
+        if (quad == 0) slot[in_tile] = m[n], slot[kRows + in_tile] = l[n];
+        continue;
+      }
+      const int token = at.q.d.begin + row / a.group, h = at.head * a.group + row % a.group;
+      T* to = reinterpret_cast<T*>(a.out + token * a.out_token_bytes + h * a.out_head_bytes);
+      const float f = l[n] == 0 ? 0 : 1 / l[n];
+#pragma unroll
+      for (int d = 0; d < kTiles; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (16 * d + 4 * quad < width) to[16 * d + 4 * quad + r] = from_float<T>(l[n] == 0 ? 0.0f : o[n][d][r] * f);
+      if (quad == 0 && a.lse) a.lse[static_cast<int64_t>(token) * a.q_heads + h] = natural_lse(m[n], l[n]);
+    }
+  } while (at.next());
+}
+
+template <class T, int ROW_BYTES, int NQ>
+void launch(const Attention& a, hipStream_t stream) {
+  constexpr int groups = groups_of<ROW_BYTES, sizeof(T)>();
+  if (a.c.width_bytes == ROW_BYTES)
+    attention_rows_kernel<T, ROW_BYTES, NQ, true><<<groups, kBlock, 0, stream>>>(a);
+  else
+    attention_rows_kernel<T, ROW_BYTES, NQ, false><<<groups, kBlock, 0, stream>>>(a);
+  launch_join<T>(a, groups, 64 * NQ, ROW_BYTES / sizeof(T), stream);
+}
+
+}  // namespace
+
+// most: more than 64 rows a tile.
+template <class T>
+void launch_many_rows(const Attention& a, bool most, hipStream_t stream) {
+  const int width = a.c.width_bytes / sizeof(T);
+  if (width <= 64) most ? launch<T, 128, 2>(a, stream) : launch<T, 128, 1>(a, stream);
+  else if (width <= 128) most ? launch<T, 256, 2>(a, stream) : launch<T, 256, 1>(a, stream);
+  else launch<T, 512, 1>(a, stream);
+}
+template void launch_many_rows<f16>(const Attention&, bool, hipStream_t);
+template void launch_many_rows<bf16>(const Attention&, bool, hipStream_t);
+
+}  // namespace spt
