@@ -26,7 +26,7 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
   do {
     const int row0 = at.tile * kRows, tokens = at.plan.end(at.q, at.tile);
     i4 qf[NQ][kChunks];
-    load_queries(a, at.q, at.head, row0, qf);
+    load_queries<T>(a, at.q, at.head, row0, qf);
     f4 o[NQ][kTiles];
     float m[NQ], l[NQ];
 #pragma unroll
@@ -38,17 +38,14 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
     }
 
     const int64_t pool = a.layer * c.layer_bytes + at.head * c.head_bytes;
-    // Where the tokens of the lane lie, -1: nowhere.
-    auto places = [&](int base, int64_t(&place)[kSub]) {
+    // Where the tokens of the lane lie: the table is read two steps ahead, and what it says is looked at one step ahead.
+    auto entries = [&](int base, int(&entry)[kSub]) {
 #pragma unroll
-      for (int u = 0; u < kSub; ++u) {
-        const int t = base + 16 * u + i;
-        place[u] = -1;
-        if (t < tokens) {
-          const int page = page_at(c, at.s, t >> c.shift);
-          if (page >= 0) place[u] = page * c.page_bytes + (t & ((1 << c.shift) - 1)) * c.slot_bytes;
-        }
-      }
+      for (int u = 0; u < kSub; ++u) entry[u] = table_entry(c, at.s, base + 16 * u + i, tokens);
+    };
+    auto places = [&](int base, const int(&entry)[kSub], int64_t(&place)[kSub]) {
+#pragma unroll
+      for (int u = 0; u < kSub; ++u) place[u] = slot_of(c, entry[u], base + 16 * u + i, tokens);
     };
     // For tokens that are nowhere the first slot of the pool is read, behind the width its last 16 bytes again: values that are put
     // aside before they count.
@@ -65,17 +62,20 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
     };
 
     char* mine = area[wave];
-    int64_t place[kSub], ahead[kSub];
+    constexpr int kApart = kWaves * kTokens;
+    int64_t place[kSub];
+    int entry[kSub];
     i4 k[kSub][kChunks], v[kSub][kChunks];
-    int base = (at.step * kWaves + wave) * kTokens;
-    const int limit = at.stop * kWaves * kTokens < tokens ? at.stop * kWaves * kTokens : tokens;
+    int base = at.step * kApart + wave * kTokens;
+    const int limit = at.stop * kApart < tokens ? at.stop * kApart : tokens;
     if (base < limit) {
-      places(base, place);
+      entries(base, entry);
+      places(base, entry, place);
+      entries(base + kApart, entry);
       load(c.K, place, k);
       load(c.V, place, v);
-      places(base + kWaves * kTokens, ahead);
     }
-    for (; base < limit; base += kWaves * kTokens) {
+    for (; base < limit; base += kApart) {
       if (!FULL)
 #pragma unroll
         for (int u = 0; u < kSub; ++u)
@@ -91,7 +91,10 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
 #pragma unroll
           for (int j = 0; j < kChunks; ++j) z[n][u] = multiply<T>(k[u][j], qf[n][j], z[n][u]);
         }
-      load(c.K, ahead, k);
+      int64_t next[kSub];
+      places(base + kApart, entry, next);
+      entries(base + 2 * kApart, entry);
+      load(c.K, next, k);
 
       // tokens of the wave that are there, and those that each row sees
       uint32_t there = 0, bad = 0, sight[NQ];
@@ -126,15 +129,15 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
       int64_t here[kSub];
 #pragma unroll
       for (int u = 0; u < kSub; ++u) here[u] = place[u];
-      load(c.V, ahead, v);
+      load(c.V, next, v);
 #pragma unroll
-      for (int u = 0; u < kSub; ++u) place[u] = ahead[u];
-      places(base + 2 * kWaves * kTokens, ahead);
+      for (int u = 0; u < kSub; ++u) place[u] = next[u];
 
       i4 p[NQ];
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
-        softmax_step(z[n], a.scale, all, &sight[n], m[n], l[n], o[n]);
+        if (!all) hide(z[n], &sight[n]);
+        softmax_step(z[n], a.scale, m[n], l[n], o[n]);
         p[n] = weights<T>(z[n]);
       }
       wave_lds_order();
@@ -212,65 +215,56 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
   } while (at.next());
 }
 
-// Joins the parts of tiles that lie in several workgroups: blockIdx.x is the workgroup that holds a tile's second part, blockIdx.y four
-// of the tile's rows; the waves share the parts.
+// Joins the parts of tiles that lie in several workgroups. blockIdx.x is a workgroup that began within a tile; those of one tile share
+// its rows, and blockIdx.y divides them further. Few parts: a wave takes a row; many: the waves of a workgroup share the parts of it.
+constexpr int kFewParts = 8;
 template <class T, int WIDTH, int ROWS>
 __global__ void __launch_bounds__(kBlock) attention_join_kernel(Attention a) {
-  __shared__ float area[kWaves][4][WIDTH];
+  constexpr int kEach = WIDTH / kWave;  // values of a lane
+  __shared__ float area[kWaves][WIDTH], sums[kWaves];
   const Part part = a.part[blockIdx.x];
-  const Drafted d = part.parts ? drafted(a.first, part.s, a.total) : Drafted{0, 0};
-  const int r0 = blockIdx.y * 4, rows = d.count * a.group - part.row - r0;
-  if (rows <= 0) return;
-  const int lane = lane_id(), wave = wave_id();
+  if (part.parts == 0) return;
+  const Drafted d = drafted(a.first, part.s, a.total);
+  const int left = d.count * a.group - part.row, rows = left < ROWS ? left : ROWS;
+  const int lane = lane_id(), wave = wave_id(), width = a.c.width_bytes / static_cast<int>(sizeof(T));
   constexpr int64_t kSlot = static_cast<int64_t>(ROWS) * (WIDTH + 2);
-  const float* from = a.partial + static_cast<int64_t>(blockIdx.x) * 2 * kSlot;  // part p > 0: slot 0 of workgroup blockIdx.x + p - 1
-  auto slot = [&](int p) { return p ? from + (p - 1) * 2 * kSlot : from - kSlot; };
-  float top[4], sum[4];
+  const float* second = a.partial + (static_cast<int64_t>(blockIdx.x) - part.place) * 2 * kSlot;  // part p > 0: slot 0 of p - 1 groups on
+  auto slot = [&](int p) { return p ? second + (p - 1) * 2 * kSlot : second - kSlot; };
+  const bool many = part.parts > kFewParts;
+  const int takers = (part.parts - 1) * gridDim.y, taker = part.place * gridDim.y + blockIdx.y;
+  for (int r = many ? taker : taker * kWaves + wave; r < rows; r += many ? takers : takers * kWaves) {
+    float top = -INFINITY, sum = 0, y[kEach] = {};
+    for (int p = lane; p < part.parts; p += kWave) top = fmaxf(top, slot(p)[r]);
+    for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+    const float zero = top == -INFINITY ? 0 : top;
+#pragma unroll 4
+    for (int p = many ? wave : 0; p < part.parts; p += many ? kWaves : 1) {
+      const float* from = slot(p);
+      const float f = exp2_of(from[r] - zero);
+      sum += f * from[ROWS + r];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) top[r] = -INFINITY, sum[r] = 0;
-  for (int p = lane; p < part.parts; p += kWave)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) top[r] = fmaxf(top[r], slot(p)[r0 + r]);
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    for (int x = 32; x; x >>= 1) top[r] = fmaxf(top[r], __shfl_xor(top[r], x));
-    for (int p = lane; p < part.parts; p += kWave)
-      sum[r] += slot(p)[ROWS + r0 + r] * exp2_of(slot(p)[r0 + r] - (top[r] == -INFINITY ? 0 : top[r]));
-    for (int x = 32; x; x >>= 1) sum[r] += __shfl_xor(sum[r], x);
-  }
-  constexpr int kEach = (WIDTH + kWave - 1) / kWave;
-  float y[4][kEach] = {};
-  for (int p = wave; p < part.parts; p += kWaves) {
-    const float* x = slot(p);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const float f = exp2_of(x[r0 + r] - (top[r] == -INFINITY ? 0 : top[r]));
-#pragma unroll
-      for (int e = 0; e < kEach; ++e)
-        if (lane + e * kWave < WIDTH) y[r][e] += f * x[2 * ROWS + (r0 + r) * WIDTH + lane + e * kWave];
+      for (int e = 0; e < kEach; ++e) y[e] += f * from[2 * ROWS + r * WIDTH + lane * kEach + e];
     }
-  }
+    if (many) {
+      __syncthreads();
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
+      for (int e = 0; e < kEach; ++e) area[wave][lane * kEach + e] = y[e];
+      if (lane == 0) sums[wave] = sum;
+      __syncthreads();
+      if (wave != 0) continue;
+      for (int w = 1; w < kWaves; ++w) {
+        sum += sums[w];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) y[e] += area[w][lane * kEach + e];
+      }
+    }
+    const int row = part.row + r, token = d.begin + row / a.group, h = part.head * a.group + row % a.group;
+    T* to = reinterpret_cast<T*>(a.out + token * a.out_token_bytes + h * a.out_head_bytes);
 #pragma unroll
     for (int e = 0; e < kEach; ++e)
-      if (lane + e * kWave < WIDTH) area[wave][r][lane + e * kWave] = y[r][e];
-  __syncthreads();
-  if (wave >= rows) return;
-  const int row = part.row + r0 + wave, token = d.begin + row / a.group, h = part.head * a.group + row % a.group;
-  float total = 0, high = 0;
-#pragma unroll
-  for (int r = 0; r < 4; ++r)
-    if (r == wave) total = sum[r], high = top[r];
-  T* to = reinterpret_cast<T*>(a.out + token * a.out_token_bytes + h * a.out_head_bytes);
-  for (int e = lane; e < a.c.width_bytes / static_cast<int>(sizeof(T)); e += kWave) {
-    float x = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) x += area[w][wave][e];
-    to[e] = from_float<T>(total == 0 ? 0.0f : x / total);
+      if (lane * kEach + e < width) to[lane * kEach + e] = from_float<T>(sum == 0 ? 0.0f : y[e] / sum);
+    if (lane == 0 && a.lse) a.lse[static_cast<int64_t>(token) * a.q_heads + h] = natural_lse(top, sum);
   }
-  if (lane == 0 && a.lse)
-    a.lse[static_cast<int64_t>(token) * a.q_heads + h] = natural_lse(high, total);
 }
 
 template <class T, int ROW_BYTES, int NQ>
@@ -295,7 +289,7 @@ void launch_few_rows(const Attention& a, hipStream_t stream) {
 
 template <class T, int WIDTH>
 void launch_join_width(const Attention& a, int groups, int rows, hipStream_t stream) {
-  const dim3 grid(groups, rows / 4);
+  const dim3 grid(groups, rows / 16);  // of a tile of two parts, four rows to a wave
   if (rows == 16) attention_join_kernel<T, WIDTH, 16><<<grid, kBlock, 0, stream>>>(a);
   else if (rows == 32) attention_join_kernel<T, WIDTH, 32><<<grid, kBlock, 0, stream>>>(a);
   else if (rows == 64) attention_join_kernel<T, WIDTH, 64><<<grid, kBlock, 0, stream>>>(a);
@@ -339,9 +333,11 @@ spt_status cache_attention_dispatch(const spt_cache* cache, int32_t layer, const
   Workspace w(ws, cache_attention_workspace(cache, q_heads));
   Part* part = w.take<Part>(kMostGroups);
   float* partial = w.take<float>(0);
+  // a scale of 0 becomes one that makes 0 of every score as well, but hidden ones stay -infinity
+  const float factor = scale == 0 ? 1e-38f : fabsf(scale) * 1.4426950408889634f;
   const Attention a{cache_view(cache), layer, total, q_heads, q_heads / cache->heads, first, pattern_view(tree),
                     static_cast<const char*>(q), static_cast<char*>(out), lse, q_token_stride * b, q_head_stride * b,
-                    out_token_stride * b, out_head_stride * b, scale * 1.4426950408889634f, part, partial};
+                    out_token_stride * b, out_head_stride * b, factor, scale < 0, part, partial};
   if (cache->dtype == SPT_F32) dispatch<float>(a, stream);
   else if (cache->dtype == SPT_F16) dispatch<f16>(a, stream);
   else dispatch<bf16>(a, stream);

@@ -32,9 +32,10 @@ using LdsQuad = __attribute__((address_space(3))) s4;
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 
-// Which part of the call a workgroup began within a tile, for the joining kernel.
+// The tile within which a workgroup began, for the joining kernel.
 struct Part {
-  int parts;  // of the tile, if this workgroup's is the second of them; else 0
+  int parts;  // of the tile; 0: the workgroup began with a tile
+  int place;  // its part is number place + 1
   int s, head, row;
 };
 
@@ -47,7 +48,8 @@ struct Attention {
   char* out;
   float* lse;
   int64_t q_token_bytes, q_head_bytes, out_token_bytes, out_head_bytes;
-  float scale;  // times log2(e)
+  float scale;  // times log2(e), positive: its sign is in the queries
+  bool negative;
   Part* part;   // of each workgroup
   float* partial;  // two slots for each workgroup: m[rows], l[rows], O[rows][width]
 };
@@ -195,11 +197,11 @@ struct Walk {
   int s, head, tile, step, steps, stop;
   int64_t left;
 
-  // False if the share is empty. Notes in `part` whether the workgroup begins with a tile's second part.
+  // False if the share is empty. Notes in `part` whether the workgroup begins within a tile.
   __device__ __forceinline__ bool start(int group, int groups, int64_t* lds, int64_t* found) {
     int64_t per = 0, at = 0, end = 0;
     const bool some = share(plan, group, groups, lds, found, per, at, end, s);
-    Part part{0, 0, 0, 0};
+    Part part{0, 0, 0, 0, 0};
     if (some) {  // `at` counts the steps of sequence s, head by head and tile by tile
       q = plan.sequence(s);
       const int64_t in_head = plan.head_steps(q);
@@ -211,7 +213,10 @@ struct Walk {
       step = static_cast<int>(rest);
       left = end - at;
       limit();
-      if (step > 0 && step <= per) part = {static_cast<int>(1 + (steps - step + per - 1) / per), s, head, tile * P::kRows};
+      if (step > 0) {
+        const int place = static_cast<int>((step - 1) / per);
+        part = {static_cast<int>(1 + (steps - (step - place * per) + per - 1) / per), place, s, head, tile * P::kRows};
+      }
     }
     if (threadIdx.x == 0) plan.a.part[group] = part;
     return some;
@@ -235,8 +240,8 @@ struct Walk {
   }
 };
 
-// Rows row0 + 16 n + i of a tile: 16 bytes of a lane from each 64 of the head, zeros behind the rows and the width.
-template <int NQ, int CHUNKS, class Q>
+// Rows row0 + 16 n + i of a tile (negated with the scale): 16 bytes of a lane from each 64 of the head, zeros behind the rows and the width.
+template <class T, int NQ, int CHUNKS, class Q>
 __device__ __forceinline__ void load_queries(const Attention& a, const Q& q, int head, int row0, i4 (&x)[NQ][CHUNKS]) {
   const int i = lane_id() & 15, quad = lane_id() >> 4, vecs = a.c.width_bytes / 16;
 #pragma unroll
@@ -247,8 +252,19 @@ __device__ __forceinline__ void load_queries(const Attention& a, const Q& q, int
     for (int j = 0; j < CHUNKS; ++j) {
       x[n][j] = i4{0, 0, 0, 0};
       if (row < q.rows && quad + 4 * j < vecs) x[n][j] = *reinterpret_cast<const i4*>(from + (quad + 4 * j) * 16);
+      if (a.negative) x[n][j] ^= sizeof(T) == 4 ? static_cast<int>(0x80000000u) : static_cast<int>(0x80008000u);
     }
   }
+}
+
+// The table's entry for token t of row s, whatever it holds; a token behind the last takes the last one's.
+__device__ __forceinline__ int table_entry(const Cache& c, int s, int t, int tokens) {
+  return c.table[static_cast<int64_t>(s) * c.row_pages + ((t < tokens ? t : tokens - 1) >> c.shift)];
+}
+// With it, once it has arrived: where the token's slot begins, -1 if it is nowhere.
+__device__ __forceinline__ int64_t slot_of(const Cache& c, int entry, int t, int tokens) {
+  if (t >= tokens || static_cast<unsigned>(entry) >= static_cast<unsigned>(c.pages)) return -1;
+  return entry * c.page_bytes + (t & ((1 << c.shift) - 1)) * c.slot_bytes;
 }
 
 // Which of the 32 tokens from `base` on a row sees, as bits; the four lanes of a row share the work and get the same.
@@ -302,35 +318,43 @@ __device__ __forceinline__ i4 turned_values(char* area, int token, int d) {
   }
 }
 
-// One step of the softmax of 16 rows: scores z (16 tokens each, 4q .. 4q+3 of a lane) become weights. seen: bits of 32 tokens each, read
-// where not all are seen.
-template <int SUB, int TILES>
-__device__ __forceinline__ void softmax_step(f4 (&z)[SUB], float scale, bool all, const uint32_t* seen, float& m, float& l, f4 (&o)[TILES]) {
+// Scores of tokens that a row does not see become -infinity. seen: bits of 32 tokens each.
+template <int SUB>
+__device__ __forceinline__ void hide(f4 (&z)[SUB], const uint32_t* seen) {
   const int quad = lane_id() >> 4;
-  float top = m;
 #pragma unroll
   for (int u = 0; u < SUB; ++u)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      z[u][r] *= scale;
-      if (!all && !(seen[u / 2] >> (16 * (u & 1) + 4 * quad + r) & 1)) z[u][r] = -INFINITY;
-      top = fmaxf(top, z[u][r]);
-    }
+    for (int r = 0; r < 4; ++r)
+      if (!(seen[u / 2] >> (16 * (u & 1) + 4 * quad + r) & 1)) z[u][r] = -INFINITY;
+}
+
+// One step of the softmax of 16 rows: scores z (16 tokens each, 4q .. 4q+3 of a lane) become weights exp2(scale z - m). What is held so
+// far is rescaled, and m raised, only when a score passes m by more than 2^kSlack in weight: most steps leave it, the weights stay
+// below 2^kSlack (f16 holds 2^16), and m cancels in the result. scale > 0.
+constexpr float kSlack = 8;
+template <int SUB, int TILES>
+__device__ __forceinline__ void softmax_step(f4 (&z)[SUB], float scale, float& m, float& l, f4 (&o)[TILES]) {
+  float top = z[0][0];
+#pragma unroll
+  for (int u = 0; u < SUB; ++u)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) top = fmaxf(top, z[u][r]);
   top = fmaxf(top, __shfl_xor(top, 16));
-  top = fmaxf(top, __shfl_xor(top, 32));
-  const float zero = top == -INFINITY ? 0 : top;
-  if (__any(top != m)) {
-    const float keep = exp2_of(m - zero);
+  top = fmaxf(top, __shfl_xor(top, 32)) * scale;
+  if (__any(top > m + kSlack)) {
+    const float high = fmaxf(m, top), keep = exp2_of(m - (high == -INFINITY ? 0 : high));
     l *= keep;
 #pragma unroll
     for (int d = 0; d < TILES; ++d) o[d] *= keep;
-    m = top;
+    m = high;
   }
+  const float zero = m == -INFINITY ? 0 : m;
 #pragma unroll
   for (int u = 0; u < SUB; ++u)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      z[u][r] = exp2_of(z[u][r] - zero);
+      z[u][r] = exp2_of(__builtin_fmaf(z[u][r], scale, -zero));
       l += z[u][r];
     }
 }

@@ -32,7 +32,7 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
     const int last = row0 + 16 * NQ < at.q.rows ? row0 + 16 * NQ - 1 : at.q.rows - 1;
     const int seen_end = row0 >= at.q.rows ? 0 : a.tree.pos ? tokens : at.q.context + last / a.group + 1;
     i4 qf[NQ][kChunks];
-    load_queries(a, at.q, at.head, row0, qf);
+    load_queries<T>(a, at.q, at.head, row0, qf);
     f4 o[NQ][kTiles];
     float m[NQ], l[NQ];
 #pragma unroll
@@ -44,55 +44,60 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
     }
 
     const int64_t pool = a.layer * c.layer_bytes + at.head * c.head_bytes;
-    int page[kLoads], page_ahead[kLoads];
+    int entry[kLoads];    // of the table, for the step behind the one that is loaded
+    uint32_t missing = 0;  // bit x: token x of the loaded step is nowhere
     i4 k[kLoads], v[kLoads];
-    auto pages = [&](int base, int(&p)[kLoads]) {
+    auto entries = [&](int base) {
 #pragma unroll
-      for (int x = 0; x < kLoads; ++x) {
-        const int t = base + token0 + x * kTokensApart;
-        p[x] = t < tokens ? page_at(c, at.s, t >> c.shift) : -1;
-      }
+      for (int x = 0; x < kLoads; ++x) entry[x] = table_entry(c, at.s, base + token0 + x * kTokensApart, tokens);
     };
     // As in the kernel for few rows: the pool's first slot for tokens that are nowhere.
     auto load = [&](int base) {
+      missing = 0;
 #pragma unroll
       for (int x = 0; x < kLoads; ++x) {
-        const int t = base + token0 + x * kTokensApart;
-        const int64_t place =
-            pool + (page[x] < 0 ? 0 : page[x] * c.page_bytes + (t & ((1 << c.shift) - 1)) * c.slot_bytes) + chunk_read * 16;
+        int64_t place = slot_of(c, entry[x], base + token0 + x * kTokensApart, tokens);
+        if (place < 0) missing |= 1u << x, place = 0;
+        place += pool + chunk_read * 16;
         k[x] = *reinterpret_cast<const i4*>(c.K + place);
         v[x] = *reinterpret_cast<const i4*>(c.V + place);
       }
     };
     // To LDS, with what the step's flags have to say of these tokens.
     auto store = [&](int base, int buffer, int flag) {
+      if (__any(missing != 0))
+#pragma unroll
+        for (int x = 0; x < kLoads; ++x)
+          if (missing >> x & 1) {
+            const int t = token0 + x * kTokensApart;
+            if (chunk == 0) atomicOr(&absent[flag][t >> 5], 1u << (t & 31));
+            v[x] = i4{0, 0, 0, 0};
+          }
+      if (base + kStep > at.q.context)
+#pragma unroll
+        for (int x = 0; x < kLoads; ++x) {
+          const int t = token0 + x * kTokensApart;
+          if (any_not_finite<T>(v[x])) atomicOr(&bad[flag][t >> 5], 1u << (t & 31));
+        }
 #pragma unroll
       for (int x = 0; x < kLoads; ++x) {
-        const int t = token0 + x * kTokensApart;
-        if (page[x] < 0) {
-          if (chunk == 0) atomicOr(&absent[flag][t >> 5], 1u << (t & 31));
-          v[x] = i4{0, 0, 0, 0};
-        } else if (base + kStep > at.q.context && any_not_finite<T>(v[x])) {
-          atomicOr(&bad[flag][t >> 5], 1u << (t & 31));
-        }
+        const int to = swizzled<ROW_BYTES>(token0 + x * kTokensApart, chunk);
         if (!FULL && chunk >= vecs) k[x] = i4{0, 0, 0, 0};
-        *reinterpret_cast<i4*>(area[0][buffer] + swizzled<ROW_BYTES>(t, chunk)) = k[x];
-        *reinterpret_cast<i4*>(area[1][buffer] + swizzled<ROW_BYTES>(t, chunk)) = v[x];
+        *reinterpret_cast<i4*>(area[0][buffer] + to) = k[x];
+        *reinterpret_cast<i4*>(area[1][buffer] + to) = v[x];
       }
     };
 
     if (threadIdx.x < 6) (&absent[0][0])[threadIdx.x] = 0, (&bad[0][0])[threadIdx.x] = 0;
     const int base0 = at.step * kStep, limit = tokens > 0 ? at.stop * kStep : base0;
     if (base0 < limit) {
-      pages(base0, page);
+      entries(base0);
       load(base0);
-      pages(base0 + kStep, page_ahead);
+      entries(base0 + kStep);
       __syncthreads();
       store(base0, 0, 0);
-#pragma unroll
-      for (int x = 0; x < kLoads; ++x) page[x] = page_ahead[x];
       load(base0 + kStep);
-      pages(base0 + 2 * kStep, page_ahead);
+      entries(base0 + 2 * kStep);
       lds_barrier();
     }
     int flag = 0, buffer = 0;
@@ -123,10 +128,8 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
         }
       if (base + kStep < limit) {
         store(base + kStep, buffer ^ 1, next_flag);
-#pragma unroll
-        for (int x = 0; x < kLoads; ++x) page[x] = page_ahead[x];
         load(base + 2 * kStep);
-        pages(base + 3 * kStep, page_ahead);
+        entries(base + 3 * kStep);
       }
       if (work) {
         const bool all = base + kStep <= at.q.context && (gone[0] | gone[1]) == 0;
@@ -139,7 +142,8 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
         i4 p[NQ][kSub / 2];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
-          softmax_step(z[n], a.scale, all, sight[n], m[n], l[n], o[n]);
+          if (!all) hide(z[n], sight[n]);
+          softmax_step(z[n], a.scale, m[n], l[n], o[n]);
 #pragma unroll
           for (int w = 0; w < kSub / 2; ++w) p[n][w] = weights<T>(&z[n][2 * w]);
         }
