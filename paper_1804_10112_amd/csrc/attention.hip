@@ -16,27 +16,14 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
   using P = Plan<kRows, kTokens * kWaves>;
   __shared__ __attribute__((aligned(16))) char area[kWaves][64 * kWidth];  // V of a wave's tokens; O of 16 rows when waves meet
   __shared__ float stat[2][kWaves][kRows];
-  __shared__ int64_t sums[kWaves], found[2];
   const Cache& c = a.c;
   const int group = xcd_contiguous_block_id(), lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), i = lane & 15,
             quad = lane >> 4, vecs = c.width_bytes / 16, width = c.width_bytes / sizeof(T);
   Walk<P> at{{a}};
-  if (!at.start(group, kGroups, sums, found)) return;
+  if (!at.start(group, kGroups)) return;
 
   do {
-    const int row0 = at.tile * kRows, tokens = at.plan.end(at.q, at.tile);
-    i4 qf[NQ][kChunks];
-    load_queries<T>(a, at.q, at.head, row0, qf);
-    f4 o[NQ][kTiles];
-    float m[NQ], l[NQ];
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      m[n] = -INFINITY;
-      l[n] = 0;
-#pragma unroll
-      for (int d = 0; d < kTiles; ++d) o[n][d] = f4{0, 0, 0, 0};
-    }
-
+    const int row0 = at.tile * kRows, tokens = at.plan.end(at.q, at.tile), common = at.plan.common(at.q, row0);
     const int64_t pool = a.layer * c.layer_bytes + at.head * c.head_bytes;
     // Where the tokens of the lane lie: the table is read two steps ahead, and what it says is looked at one step ahead.
     auto entries = [&](int base, int(&entry)[kSub]) {
@@ -65,15 +52,26 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
     constexpr int kApart = kWaves * kTokens;
     int64_t place[kSub];
     int entry[kSub];
-    i4 k[kSub][kChunks], v[kSub][kChunks];
+    i4 qf[NQ][kChunks], k[kSub][kChunks], v[kSub][kChunks];
     int base = at.step * kApart + wave * kTokens;
     const int limit = at.stop * kApart < tokens ? at.stop * kApart : tokens;
     if (base < limit) {
       entries(base, entry);
+      load_queries<16>(a, at.q, at.head, row0, qf);
       places(base, entry, place);
       entries(base + kApart, entry);
       load(c.K, place, k);
       load(c.V, place, v);
+      finish_queries<T, FULL>(a, qf);
+    }
+    f4 o[NQ][kTiles];
+    float m[NQ], l[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      m[n] = -INFINITY;
+      l[n] = 0;
+#pragma unroll
+      for (int d = 0; d < kTiles; ++d) o[n][d] = f4{0, 0, 0, 0};
     }
     for (; base < limit; base += kApart) {
       if (!FULL)
@@ -100,11 +98,11 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
       uint32_t there = 0, bad = 0, sight[NQ];
 #pragma unroll
       for (int u = 0; u < kSub; ++u) there |= static_cast<uint32_t>(__ballot(place[u] >= 0) & 0xffff) << (16 * u);
-      const bool all = base + kTokens <= at.q.context && there == low_bits(kTokens);
+      const bool all = base + kTokens <= common && there == low_bits(kTokens);
       if (!all) {
 #pragma unroll
         for (int n = 0; n < NQ; ++n) sight[n] = row_sight(a, at.q, row0 + 16 * n + i, base) & there;
-        if (base + kTokens > at.q.context) {  // tokens that some rows see and others do not
+        if (base + kTokens > common) {  // tokens that some rows see and others do not
 #pragma unroll
           for (int u = 0; u < kSub; ++u) {
             bool odd = false;
@@ -133,13 +131,13 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
 #pragma unroll
       for (int u = 0; u < kSub; ++u) place[u] = next[u];
 
+      if (!all)
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) hide(z[n], &sight[n]);
+      softmax_step(z, a.scale, m, l, o);
       i4 p[NQ];
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        if (!all) hide(z[n], &sight[n]);
-        softmax_step(z[n], a.scale, m[n], l[n], o[n]);
-        p[n] = weights<T>(z[n]);
-      }
+      for (int n = 0; n < NQ; ++n) p[n] = weights<T>(z[n]);
       wave_lds_order();
 #pragma unroll
       for (int d = 0; d < kTiles; ++d) {
@@ -170,8 +168,7 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
     // the waves meet
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-      l[n] += __shfl_xor(l[n], 16);
-      l[n] += __shfl_xor(l[n], 32);
+      l[n] = sum_of_row(l[n]);
       if (quad == 0) stat[0][wave][16 * n + i] = m[n], stat[1][wave][16 * n + i] = l[n];
     }
     __syncthreads();
@@ -202,7 +199,7 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
           *reinterpret_cast<f4*>(slot + 2 * kRows + (16 * n + r) * kWidth + 4 * e) = y;
           if (e == 0) slot[16 * n + r] = high, slot[kRows + 16 * n + r] = sum;
         } else if (row < at.q.rows) {
-          const int token = at.q.d.begin + row / a.group, h = at.head * a.group + row % a.group;
+          const int token = at.q.d.begin + row / a.by_group, h = at.head * a.group + row - (token - at.q.d.begin) * a.group;
           T* to = reinterpret_cast<T*>(a.out + token * a.out_token_bytes + h * a.out_head_bytes) + 4 * e;
 #pragma unroll
           for (int b = 0; b < 4; ++b)
@@ -258,7 +255,7 @@ __global__ void __launch_bounds__(kBlock) attention_join_kernel(Attention a) {
         for (int e = 0; e < kEach; ++e) y[e] += area[w][lane * kEach + e];
       }
     }
-    const int row = part.row + r, token = d.begin + row / a.group, h = part.head * a.group + row % a.group;
+    const int row = part.row + r, token = d.begin + row / a.by_group, h = part.head * a.group + row - (token - d.begin) * a.group;
     T* to = reinterpret_cast<T*>(a.out + token * a.out_token_bytes + h * a.out_head_bytes);
 #pragma unroll
     for (int e = 0; e < kEach; ++e)
@@ -335,7 +332,7 @@ spt_status cache_attention_dispatch(const spt_cache* cache, int32_t layer, const
   float* partial = w.take<float>(0);
   // a scale of 0 becomes one that makes 0 of every score as well, but hidden ones stay -infinity
   const float factor = scale == 0 ? 1e-38f : fabsf(scale) * 1.4426950408889634f;
-  const Attention a{cache_view(cache), layer, total, q_heads, q_heads / cache->heads, first, pattern_view(tree),
+  const Attention a{cache_view(cache), layer, total, q_heads, q_heads / cache->heads, divisor(q_heads / cache->heads), first, pattern_view(tree),
                     static_cast<const char*>(q), static_cast<char*>(out), lse, q_token_stride * b, q_head_stride * b,
                     out_token_stride * b, out_head_stride * b, factor, scale < 0, part, partial};
   if (cache->dtype == SPT_F32) dispatch<float>(a, stream);

@@ -42,6 +42,7 @@ struct Part {
 struct Attention {
   Cache c;
   int layer, total, q_heads, group;
+  Divisor by_group;
   const int32_t* first;
   Pattern tree;  // pos NULL: each token sees those up to itself
   const char* q;
@@ -116,8 +117,12 @@ struct Plan {
   __device__ __forceinline__ int end(const Sequence& q, int tile) const {
     if (a.tree.pos) return q.length;
     const int last = (tile + 1) * ROWS < q.rows ? (tile + 1) * ROWS - 1 : q.rows - 1;
-    const int e = q.context + last / a.group + 1;
+    const int e = q.context + last / a.by_group + 1;
     return e > 0 ? e : 0;
+  }
+  // Tokens that every row from `row` on sees.
+  __device__ __forceinline__ int common(const Sequence& q, int row) const {
+    return a.tree.pos ? q.context : q.context + row / a.by_group + 1;
   }
   __device__ __forceinline__ int steps(const Sequence& q, int tile) const {
     const int e = end(q, tile);
@@ -132,58 +137,46 @@ struct Plan {
   }
 };
 
-__device__ __forceinline__ int64_t block_inclusive_scan(int64_t v, int64_t* lds) {
-  const int lane = lane_id(), wave = wave_id();
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const int64_t o = __shfl_up(static_cast<long long>(v), d);
-    if (lane >= d) v += o;
-  }
-  __syncthreads();
-  if (lane == kWave - 1) lds[wave] = v;
-  __syncthreads();
-  for (int w = 0; w < wave; ++w) v += lds[w];
-  return v;
+__device__ __forceinline__ int64_t lane_value(int64_t v, int lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(v), lane), hi = __builtin_amdgcn_readlane(static_cast<int>(v >> 32), lane);
+  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
 }
 
-// Finds the sequence that the workgroup's share begins in: `begin` becomes the steps before it within the sequence. All threads of
-// the workgroup; false if the share is empty.
+// Finds the sequence that the workgroup's share of `groups` (a power of two) begins in; begin and end count the steps within it. False if
+// the share is empty. Every wave does all of it, 64 sequences at a time, so that none waits for another.
 template <class P>
-__device__ __forceinline__ bool share(const P& plan, int group, int groups, int64_t* lds, int64_t* found, int64_t& per, int64_t& begin, int64_t& end,
-                                      int& s) {
-  const int rows = plan.a.c.rows, heads = plan.a.c.heads;
+__device__ __forceinline__ bool share(const P& plan, int group, int groups, int64_t& per, int64_t& begin, int64_t& end, int& s) {
+  const int rows = plan.a.c.rows, heads = plan.a.c.heads, lane = lane_id();
   int64_t total = 0, mine = 0, upto = 0;
-  for (int base = 0; base < rows; base += kBlock) {
-    const int r = base + threadIdx.x;
+  auto count = [&](int base) {
+    const int r = base + lane;
     mine = r < rows ? plan.head_steps(plan.sequence(r)) * heads : 0;
-    upto = total + block_inclusive_scan(mine, lds);
-    __syncthreads();
-    if (threadIdx.x == kBlock - 1) lds[0] = upto;
-    __syncthreads();
-    total = lds[0];
-    __syncthreads();
-  }
-  per = (total + groups - 1) / groups;
+    upto = mine;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+      const int64_t o = __shfl_up(static_cast<long long>(upto), d);
+      if (lane >= d) upto += o;
+    }
+    upto += total;
+    total = lane_value(upto, kWave - 1);
+  };
+  for (int base = 0; base < rows; base += kWave) count(base);
+  per = (total + groups - 1) >> (31 - __builtin_clz(groups));
   begin = group * per;
   end = begin + per < total ? begin + per : total;
   if (begin >= end) return false;
-  int64_t before = 0;
-  for (int base = 0; base < rows; base += kBlock) {
-    const int r = base + threadIdx.x;
-    if (rows > kBlock) {
-      mine = r < rows ? plan.head_steps(plan.sequence(r)) * heads : 0;
-      upto = before + block_inclusive_scan(mine, lds);
+  total = 0;
+  int base = 0;
+  if (rows > kWave) {
+    count(0);
+    while (total <= begin) {
+      base += kWave;
+      count(base);
     }
-    if (upto > begin && upto - mine <= begin) found[0] = r, found[1] = upto - mine;
-    __syncthreads();
-    if (threadIdx.x == kBlock - 1) lds[0] = upto;
-    __syncthreads();
-    before = lds[0];
-    __syncthreads();
-    if (before > begin) break;
   }
-  s = __builtin_amdgcn_readfirstlane(static_cast<int>(found[0]));
-  const int64_t skipped = found[1];
+  const int found = __builtin_ctzll(__ballot(upto > begin));
+  const int64_t skipped = lane_value(upto - mine, found);
+  s = base + found;
   begin -= skipped;
   end -= skipped;
   return true;
@@ -198,14 +191,14 @@ struct Walk {
   int64_t left;
 
   // False if the share is empty. Notes in `part` whether the workgroup begins within a tile.
-  __device__ __forceinline__ bool start(int group, int groups, int64_t* lds, int64_t* found) {
+  __device__ __forceinline__ bool start(int group, int groups) {
     int64_t per = 0, at = 0, end = 0;
-    const bool some = share(plan, group, groups, lds, found, per, at, end, s);
+    const bool some = share(plan, group, groups, per, at, end, s);
     Part part{0, 0, 0, 0, 0};
     if (some) {  // `at` counts the steps of sequence s, head by head and tile by tile
       q = plan.sequence(s);
       const int64_t in_head = plan.head_steps(q);
-      head = static_cast<int>(at / in_head);
+      head = (at | in_head) >> 32 ? static_cast<int>(at / in_head) : static_cast<int>(static_cast<uint32_t>(at) / static_cast<uint32_t>(in_head));
       tile = 0;
       int64_t rest = at - head * in_head;
       steps = plan.steps(q, 0);
@@ -214,8 +207,8 @@ struct Walk {
       left = end - at;
       limit();
       if (step > 0) {
-        const int place = static_cast<int>((step - 1) / per);
-        part = {static_cast<int>(1 + (steps - (step - place * per) + per - 1) / per), place, s, head, tile * P::kRows};
+        const int each = per < steps ? static_cast<int>(per) : steps, place = (step - 1) / each;
+        part = {1 + (steps - (step - place * each) + each - 1) / each, place, s, head, tile * P::kRows};
       }
     }
     if (threadIdx.x == 0) plan.a.part[group] = part;
@@ -240,21 +233,32 @@ struct Walk {
   }
 };
 
-// Rows row0 + 16 n + i of a tile (negated with the scale): 16 bytes of a lane from each 64 of the head, zeros behind the rows and the width.
-template <class T, int NQ, int CHUNKS, class Q>
+// Rows row0 + APART n + i of a tile, for those behind the last the last one: 16 bytes of a lane from each 64 of the head.
+template <int APART, int NQ, int CHUNKS, class Q>
 __device__ __forceinline__ void load_queries(const Attention& a, const Q& q, int head, int row0, i4 (&x)[NQ][CHUNKS]) {
   const int i = lane_id() & 15, quad = lane_id() >> 4, vecs = a.c.width_bytes / 16;
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
-    const int row = row0 + 16 * n + i, token = row / a.group;
+    const int r = row0 + APART * n + i, row = r < q.rows ? r : q.rows - 1, token = row / a.by_group;
     const char* from = a.q + (q.d.begin + token) * a.q_token_bytes + (head * a.group + row - token * a.group) * a.q_head_bytes;
 #pragma unroll
     for (int j = 0; j < CHUNKS; ++j) {
-      x[n][j] = i4{0, 0, 0, 0};
-      if (row < q.rows && quad + 4 * j < vecs) x[n][j] = *reinterpret_cast<const i4*>(from + (quad + 4 * j) * 16);
-      if (a.negative) x[n][j] ^= sizeof(T) == 4 ? static_cast<int>(0x80000000u) : static_cast<int>(0x80008000u);
+      const int chunk = quad + 4 * j;
+      x[n][j] = *reinterpret_cast<const i4*>(from + (chunk < vecs ? chunk : vecs - 1) * 16);
     }
   }
+}
+// Before they are used: zeros behind the width, and the sign of the scale.
+template <class T, bool FULL, int NQ, int CHUNKS>
+__device__ __forceinline__ void finish_queries(const Attention& a, i4 (&x)[NQ][CHUNKS]) {
+  const int quad = lane_id() >> 4, vecs = a.c.width_bytes / 16;
+#pragma unroll
+  for (int n = 0; n < NQ; ++n)
+#pragma unroll
+    for (int j = 0; j < CHUNKS; ++j) {
+      if (!FULL && quad + 4 * j >= vecs) x[n][j] = i4{0, 0, 0, 0};
+      if (a.negative) x[n][j] ^= sizeof(T) == 4 ? static_cast<int>(0x80000000u) : static_cast<int>(0x80008000u);
+    }
 }
 
 // The table's entry for token t of row s, whatever it holds; a token behind the last takes the last one's.
@@ -264,13 +268,14 @@ __device__ __forceinline__ int table_entry(const Cache& c, int s, int t, int tok
 // With it, once it has arrived: where the token's slot begins, -1 if it is nowhere.
 __device__ __forceinline__ int64_t slot_of(const Cache& c, int entry, int t, int tokens) {
   if (t >= tokens || static_cast<unsigned>(entry) >= static_cast<unsigned>(c.pages)) return -1;
-  return entry * c.page_bytes + (t & ((1 << c.shift) - 1)) * c.slot_bytes;
+  return static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(entry)) * c.page_vecs +
+                              static_cast<uint64_t>(static_cast<uint32_t>(t & ((1 << c.shift) - 1))) * c.slot_vecs) << 4;
 }
 
 // Which of the 32 tokens from `base` on a row sees, as bits; the four lanes of a row share the work and get the same.
 template <class Q>
 __device__ __forceinline__ uint32_t row_sight(const Attention& a, const Q& q, int row, int base) {
-  const int quad = lane_id() >> 4, token = row / a.group;
+  const int quad = lane_id() >> 4, token = row / a.by_group;
   uint32_t bits = low_bits(q.context - base);
   if (row >= q.rows) {
     bits = 0;
@@ -329,34 +334,59 @@ __device__ __forceinline__ void hide(f4 (&z)[SUB], const uint32_t* seen) {
       if (!(seen[u / 2] >> (16 * (u & 1) + 4 * quad + r) & 1)) z[u][r] = -INFINITY;
 }
 
-// One step of the softmax of 16 rows: scores z (16 tokens each, 4q .. 4q+3 of a lane) become weights exp2(scale z - m). What is held so
-// far is rescaled, and m raised, only when a score passes m by more than 2^kSlack in weight: most steps leave it, the weights stay
-// below 2^kSlack (f16 holds 2^16), and m cancels in the result. scale > 0.
+// The largest, and the sum, over the four lanes that hold a row (lane, lane ^ 16, lane ^ 32, lane ^ 48): swapping the odd rows of 16
+// lanes of one register with the even rows of another leaves both neighbours' values in the two.
+__device__ __forceinline__ float max_of_row(float x) {
+  auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float sum_of_row(float x) {
+  auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+
+// One step of the softmax of 16 rows each: scores z (16 tokens each, 4q .. 4q+3 of a lane) become weights exp2(scale z - m). What is
+// held so far is rescaled, and m raised, only when a score passes m by more than 2^kSlack in weight: most steps leave it, the weights
+// stay below 2^kSlack (f16 holds 2^16), and m cancels in the result. scale > 0.
 constexpr float kSlack = 8;
-template <int SUB, int TILES>
-__device__ __forceinline__ void softmax_step(f4 (&z)[SUB], float scale, float& m, float& l, f4 (&o)[TILES]) {
-  float top = z[0][0];
+template <int COUNT, int NQ, int SUB, int TILES>
+__device__ __forceinline__ void softmax_step(f4 (&z)[COUNT][SUB], float scale, float (&m)[NQ], float (&l)[NQ], f4 (&o)[NQ][TILES]) {
+  float top[COUNT];
+  bool grown = false;
 #pragma unroll
-  for (int u = 0; u < SUB; ++u)
+  for (int n = 0; n < COUNT; ++n) {
+    top[n] = z[n][0][0];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) top = fmaxf(top, z[u][r]);
-  top = fmaxf(top, __shfl_xor(top, 16));
-  top = fmaxf(top, __shfl_xor(top, 32)) * scale;
-  if (__any(top > m + kSlack)) {
-    const float high = fmaxf(m, top), keep = exp2_of(m - (high == -INFINITY ? 0 : high));
-    l *= keep;
+    for (int u = 0; u < SUB; ++u)
 #pragma unroll
-    for (int d = 0; d < TILES; ++d) o[d] *= keep;
-    m = high;
+      for (int r = 0; r < 4; ++r) top[n] = fmaxf(top[n], z[n][u][r]);
+    top[n] = max_of_row(top[n]) * scale;
+    grown |= top[n] > m[n] + kSlack;
   }
-  const float zero = m == -INFINITY ? 0 : m;
+  if (__any(grown))
 #pragma unroll
-  for (int u = 0; u < SUB; ++u)
+    for (int n = 0; n < COUNT; ++n) {
+      const float high = fmaxf(m[n], top[n]), keep = exp2_of(m[n] - (high == -INFINITY ? 0 : high));
+      l[n] *= keep;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      z[u][r] = exp2_of(__builtin_fmaf(z[u][r], scale, -zero));
-      l += z[u][r];
+      for (int d = 0; d < TILES; ++d) o[n][d] *= keep;
+      m[n] = high;
     }
+#pragma unroll
+  for (int n = 0; n < COUNT; ++n) {
+    const float zero = m[n] == -INFINITY ? 0 : m[n];
+#pragma unroll
+    for (int u = 0; u < SUB; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        z[n][u][r] = exp2_of(__builtin_fmaf(z[n][u][r], scale, -zero));
+        l[n] += z[n][u][r];
+      }
+  }
 }
 
 // The weights of 32 tokens (16 of float32) as an operand. They are rounded to the values' type, which the matrix instruction takes:

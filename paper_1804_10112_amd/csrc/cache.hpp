@@ -13,6 +13,7 @@ struct Cache {
   int64_t layer_bytes, page_bytes, slot_bytes, head_bytes;
   int rows, row_pages, pages, shift;  // page = 1 << shift
   int layers, heads, width_bytes;
+  uint32_t page_vecs, slot_vecs;  // page_bytes and slot_bytes in units of 16
 };
 
 inline int value_bytes(int dtype) { return dtype == SPT_F32 ? 4 : 2; }
@@ -23,7 +24,7 @@ inline Cache cache_view(const spt_cache* c) {
   while ((1 << shift) < c->page) ++shift;
   return {static_cast<char*>(c->K), static_cast<char*>(c->V), c->table, c->len, c->refs, c->layer_stride * b, c->page_stride * b,
           c->slot_stride * b, c->head_stride * b, c->rows, c->row_pages, static_cast<int>(c->pages), shift, c->layers, c->heads,
-          static_cast<int>(c->width * b)};
+          static_cast<int>(c->width * b), static_cast<uint32_t>(c->page_stride * b / 16), static_cast<uint32_t>(c->slot_stride * b / 16)};
 }
 
 // A CSR pattern: the entries of row r are crd[begin(r) .. end(r)), whatever pos holds.
@@ -37,7 +38,23 @@ inline Pattern pattern_view(const spt_tensor* t) {
   return t ? Pattern{t->level[1].pos, t->level[1].crd, static_cast<int>(t->nvals)} : Pattern{nullptr, nullptr, 0};
 }
 
+// Division of numbers from 0 to 2^31 - 1 by a divisor that the host knows: one multiplication. With 2^shift the next power of two from
+// the divisor d on and mul = ceil(2^(31 + shift) / d), mul d exceeds 2^(31 + shift) by less than 2^shift, so x mul / 2^(31 + shift)
+// exceeds x / d by less than 1 / d.
+struct Divisor {
+  uint32_t mul, shift;
+};
+inline Divisor divisor(uint32_t d) {
+  uint32_t shift = 0;
+  while ((uint64_t(1) << shift) < d) ++shift;
+  return {static_cast<uint32_t>(((uint64_t(1) << (31 + shift)) + d - 1) / d), shift};
+}
+
 #if defined(__HIPCC__)
+
+__device__ __forceinline__ int operator/(int x, const Divisor& d) {
+  return static_cast<int>(__umulhi(static_cast<uint32_t>(x) << 1, d.mul) >> d.shift);
+}
 
 __host__ __device__ __forceinline__ int clamped(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
 

@@ -21,7 +21,7 @@ spt_status adjust_logits_dispatch(int32_t dtype, int64_t R, int64_t V, const voi
                                   const spt_logit_rules* rules, void* out, int64_t out_stride, hipStream_t s);
 
 // Limits that keep grids and 32-bit indices of the kernels in range.
-constexpr int64_t kMaxRows = 1 << 20, kMaxTokens = 1 << 24, kMaxForks = 1 << 16, kMaxStride = int64_t(1) << 40;
+constexpr int64_t kMaxRows = 1 << 20, kMaxTokens = 1 << 24, kMaxForks = 1 << 16, kMaxStride = int64_t(1) << 40, kMaxInPage = int64_t(1) << 33;
 
 static bool narrow_type(int32_t dtype, const char* what) {
   if (dtype == SPT_F32 || dtype == SPT_F16 || dtype == SPT_BF16) return true;
@@ -59,6 +59,8 @@ static spt_status cache_ok(const spt_cache* c, const char* what) {
   if (!stride_ok(c->layer_stride, c->dtype) || !stride_ok(c->page_stride, c->dtype) || !stride_ok(c->slot_stride, c->dtype) ||
       !stride_ok(c->head_stride, c->dtype))
     return fail(SPT_ERR_INVALID_ARG, "%s: the cache's strides must not be negative and must be multiples of 16 bytes", what);
+  if (c->page_stride >= kMaxInPage || c->slot_stride >= kMaxInPage || c->head_stride >= kMaxInPage)
+    return fail(SPT_ERR_UNSUPPORTED, "%s: a page, slot or head stride of 2^33 elements or more", what);
   if (c->pages > 0 && (!c->K || !c->V || !c->refs)) return fail(SPT_ERR_INVALID_ARG, "%s: K, V or refs is null", what);
   if (odd_address(c->K) || odd_address(c->V)) return fail(SPT_ERR_INVALID_ARG, "%s: K or V is not 16-byte aligned", what);
   if (c->rows > 0 && (!c->len || (!c->table && c->row_pages > 0)))
