@@ -463,7 +463,8 @@ spt_status spt_validate(const spt_tensor* T, int32_t* err_dev, void* stream);
  *   page       slots of a page: a power of two, 1 .. 65536
  *   rows       <= 2^20; row_pages: places of a row of the table
  *   pages      < 2^31 - 1; rows * (row_pages + 1) < 2^31 - 1; page * row_pages < 2^31 - 65537
- *   strides    in elements, not negative, multiples of 16 bytes; K and V are 16-byte aligned
+ *   strides    in elements, not negative, multiples of 16 bytes, below 2^40 (layer) and 2^33; K and V are
+ *              16-byte aligned
  * table, len and refs are read and written by the entry points that say so; the struct itself is read only
  * during the call, on the host. Like every call they enqueue kernels and return; all sizes that change from
  * step to step are on the device, so a step can be captured in a graph and replayed.
@@ -575,7 +576,7 @@ size_t spt_cache_workspace_bytes(int32_t op, const spt_cache* c, int32_t q_heads
  *   bias        CSR, sequences x V, SPT_F32, columns unique in a row; NULL: none
  *   allowed     device uint32, R rows of allowed_stride words: bit v % 32 of word v / 32; NULL: all are
  * logits and out may be the same array. dtype SPT_F32, SPT_F16 or SPT_BF16; row strides in elements, >= V;
- * V < 2^31 - 1, R and sequences <= 2^24. Needs no workspace.
+ * V <= 2^27, R and sequences <= 2^24. Needs no workspace.
  */
 typedef struct {
   const int32_t* first;

@@ -21,7 +21,8 @@ spt_status adjust_logits_dispatch(int32_t dtype, int64_t R, int64_t V, const voi
                                   const spt_logit_rules* rules, void* out, int64_t out_stride, hipStream_t s);
 
 // Limits that keep grids and 32-bit indices of the kernels in range.
-constexpr int64_t kMaxRows = 1 << 20, kMaxTokens = 1 << 24, kMaxForks = 1 << 16, kMaxStride = int64_t(1) << 40, kMaxInPage = int64_t(1) << 33;
+constexpr int64_t kMaxRows = 1 << 20, kMaxTokens = 1 << 24, kMaxForks = 1 << 16, kMaxStride = int64_t(1) << 40, kMaxInPage = int64_t(1) << 33,
+                  kMaxColumns = 1 << 27;
 
 static bool narrow_type(int32_t dtype, const char* what) {
   if (dtype == SPT_F32 || dtype == SPT_F16 || dtype == SPT_BF16) return true;
@@ -215,6 +216,8 @@ spt_status spt_adjust_logits(int32_t dtype, int64_t R, int64_t V, const void* lo
   if (R > kMaxTokens || rules->sequences > kMaxTokens)
     return fail(SPT_ERR_UNSUPPORTED, "adjust_logits: %lld rows, %lld sequences, at most %lld", (long long)R,
                 (long long)rules->sequences, (long long)kMaxTokens);
+  if (V > kMaxColumns)
+    return fail(SPT_ERR_UNSUPPORTED, "adjust_logits: %lld columns, at most %lld", (long long)V, (long long)kMaxColumns);
   if (!rules->first && R != rules->sequences)
     return fail(SPT_ERR_INVALID_ARG, "adjust_logits: %lld rows of %lld sequences need first", (long long)R,
                 (long long)rules->sequences);

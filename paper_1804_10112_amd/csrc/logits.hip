@@ -19,54 +19,172 @@ struct Logits {
   const uint32_t* allowed;
 };
 
-constexpr int kSegment = 8192;  // columns of a workgroup
+constexpr int kThreads = 512;
 
-// A workgroup takes a row and a segment of the columns: the counts and the biases of the segment are collected in LDS, then the
-// row's logits go through once.
 template <class T>
-__global__ void __launch_bounds__(kBlock) logits_kernel(Logits a) {
-  __shared__ int count[kSegment];
-  __shared__ float bias[kSegment];
-  const int r = blockIdx.x, lo = blockIdx.y * kSegment, n = a.cols - lo < kSegment ? a.cols - lo : kSegment;
-  int s = r, begin = r;
+struct Values {
+  T v[Vec16<T>::n];
+};
+
+constexpr int kKept = 8;            // tokens of the sequence that a thread holds in registers; the others are read again for each segment
+constexpr int kNowhere = -(1 << 30);  // below every segment
+
+// A workgroup takes segments of a row, VECS times 16 bytes a thread, counted from where the row is aligned: blockIdx.y, blockIdx.y +
+// gridDim.y, .. In LDS lie the counts of a segment's columns and their biases: integer counts and unique biases, so nothing depends on an
+// order. The sequence's tokens are read at once, into registers, and each segment picks its own; the logits of the next segment are
+// under way while one is counted. A thread clears the counts that it has read, so a segment takes two barriers.
+template <class T, int VECS, bool BIAS>
+__global__ void __launch_bounds__(kThreads) logits_kernel(Logits a) {
+  constexpr int n = Vec16<T>::n, kSegment = kThreads * VECS * n;
+  __shared__ __attribute__((aligned(16))) int count[kSegment];
+  __shared__ __attribute__((aligned(16))) float bias[BIAS ? kSegment : 4];
+  const int r = blockIdx.x;
+  const T* in = static_cast<const T*>(a.in) + r * a.in_stride;
+  T* out = static_cast<T*>(a.out) + r * a.out_stride;
+  const int ahead = static_cast<int>(-reinterpret_cast<intptr_t>(in) / static_cast<int>(sizeof(T))) & (n - 1);
+  int lo = (ahead ? ahead - n : 0) + static_cast<int>(blockIdx.y) * kSegment;  // column of the segment's first value
+  if (lo >= a.cols) return;
+  int s = r, begin = r, last = r + 1;
   if (a.first) {
     s = wave_row_of(a.first, a.sequences, r);
     if (s < 0) return;
     begin = clamped(a.first[s], 0, a.rows);
+    last = clamped(a.first[s + 1], 0, a.rows);
   }
-  for (int v = threadIdx.x; v < n; v += kBlock) count[v] = 0, bias[v] = 0;
-  __syncthreads();
-  if (a.seen.pos)
-    for (int e = pattern_begin(a.seen, s) + threadIdx.x; e < pattern_end(a.seen, s); e += kBlock) {
-      const unsigned v = static_cast<unsigned>(a.seen.crd[e]) - lo;
-      if (v < static_cast<unsigned>(n)) atomicAdd(&count[v], 1);
+  const bool aligned = (reinterpret_cast<uintptr_t>(out + ahead) & 15) == 0;
+  Values<T> x[VECS];
+  auto load = [&](int from) {
+#pragma unroll
+    for (int k = 0; k < VECS; ++k) {
+      const int v = from + (k * kThreads + threadIdx.x) * n;
+      if (v >= 0 && v + n <= a.cols) {
+        x[k] = *reinterpret_cast<const Values<T>*>(__builtin_assume_aligned(in + v, 16));
+      } else {
+#pragma unroll
+        for (int e = 0; e < n; ++e)
+          if (v + e >= 0 && v + e < a.cols) x[k].v[e] = in[v + e];
+      }
     }
-  if (a.drafts) {
-    const int x0 = a.tree.pos ? pattern_begin(a.tree, r) : begin, x1 = a.tree.pos ? pattern_end(a.tree, r) : r + 1;
-    const int end = a.first ? clamped(a.first[s + 1], 0, a.rows) : r + 1;
-    for (int e = x0 + threadIdx.x; e < x1; e += kBlock) {
-      const int64_t node = a.tree.pos ? static_cast<int64_t>(begin) + a.tree.crd[e] : e;
-      if (node < begin || node >= end) continue;
-      const unsigned v = static_cast<unsigned>(a.drafts[node]) - lo;
-      if (v < static_cast<unsigned>(n)) atomicAdd(&count[v], 1);
-    }
-  }
-  if (a.bias.pos)
-    for (int e = pattern_begin(a.bias, s) + threadIdx.x; e < pattern_end(a.bias, s); e += kBlock) {
-      const unsigned v = static_cast<unsigned>(a.bias.crd[e]) - lo;
-      if (v < static_cast<unsigned>(n)) bias[v] = a.bias_vals[e];
-    }
-  __syncthreads();
+  };
+  load(lo);
+  auto column = [&](int v) { return v >= 0 && v < a.cols ? v : kNowhere; };
+  auto way_token = [&](int e) {  // of entry e of the row's way
+    const int64_t node = a.tree.pos ? static_cast<int64_t>(begin) + a.tree.crd[e] : e;
+    return node >= begin && node < last ? column(a.drafts[node]) : kNowhere;
+  };
+  const int seen0 = a.seen.pos ? pattern_begin(a.seen, s) : 0, seen1 = a.seen.pos ? pattern_end(a.seen, s) : 0;
+  const int bias0 = BIAS ? pattern_begin(a.bias, s) : 0, bias1 = BIAS ? pattern_end(a.bias, s) : 0;
+  const int way0 = !a.drafts ? 0 : a.tree.pos ? pattern_begin(a.tree, r) : begin;
+  const int way1 = !a.drafts ? 0 : a.tree.pos ? pattern_end(a.tree, r) : r + 1;
+  const int t = threadIdx.x;
+  int token[kKept], way = kNowhere, at_bias = kNowhere;
+  float bias_value = 0;
+#pragma unroll
+  for (int k = 0; k < kKept; ++k) token[k] = seen0 + k * kThreads + t < seen1 ? a.seen.crd[seen0 + k * kThreads + t] : kNowhere;
+  if (way0 + t < way1) way = way_token(way0 + t);
+  if (BIAS && bias0 + t < bias1) at_bias = column(a.bias.crd[bias0 + t]), bias_value = a.bias_vals[bias0 + t];
   const float rep = a.repetition ? a.repetition[s] : 1, pres = a.presence ? a.presence[s] : 0, freq = a.frequency ? a.frequency[s] : 0;
-  const T* in = static_cast<const T*>(a.in) + r * a.in_stride + lo;
-  T* out = static_cast<T*>(a.out) + r * a.out_stride + lo;
-  for (int v = threadIdx.x; v < n; v += kBlock) {
-    float x = to_float(in[v]);
-    if (count[v] > 0) x = (x > 0 ? x / rep : x * rep) - (pres + freq * static_cast<float>(count[v]));
-    x += bias[v];
-    if (a.allowed && !(a.allowed[r * a.allowed_stride + ((lo + v) >> 5)] >> ((lo + v) & 31) & 1)) x = -INFINITY;
-    out[v] = from_float<T>(x);
+  const uint32_t* allowed = a.allowed ? a.allowed + r * a.allowed_stride : nullptr;
+  for (int k = t; k < kSegment / 4; k += kThreads) {
+    reinterpret_cast<int4*>(count)[k] = int4{0, 0, 0, 0};
+    if (BIAS) reinterpret_cast<float4*>(bias)[k] = float4{0, 0, 0, 0};
   }
+#pragma unroll
+  for (int k = 0; k < kKept; ++k) token[k] = column(token[k]);
+  lds_barrier();
+
+  while (true) {
+    const unsigned width = a.cols - lo < kSegment ? a.cols - lo : kSegment;
+    auto add = [&](int v) {
+      if (static_cast<unsigned>(v - lo) < width) atomicAdd(&count[v - lo], 1);
+    };
+#pragma unroll
+    for (int k = 0; k < kKept; ++k) add(token[k]);
+    for (int e = seen0 + kKept * kThreads + t; e < seen1; e += kThreads) add(column(a.seen.crd[e]));
+    add(way);
+    for (int e = way0 + kThreads + t; e < way1; e += kThreads) add(way_token(e));
+    if (BIAS) {
+      if (static_cast<unsigned>(at_bias - lo) < width) bias[at_bias - lo] = bias_value;
+      for (int e = bias0 + kThreads + t; e < bias1; e += kThreads) {
+        const int v = column(a.bias.crd[e]);
+        if (static_cast<unsigned>(v - lo) < width) bias[v - lo] = a.bias_vals[e];
+      }
+    }
+    Values<T> now[VECS];
+#pragma unroll
+    for (int k = 0; k < VECS; ++k) now[k] = x[k];
+    const int64_t following = static_cast<int64_t>(lo) + static_cast<int64_t>(gridDim.y) * kSegment;
+    const bool more = following < a.cols;
+    if (more) load(static_cast<int>(following));
+    lds_barrier();
+#pragma unroll
+    for (int k = 0; k < VECS; ++k) {
+      const int at = (k * kThreads + t) * n, v = lo + at;
+      if (v >= a.cols) break;
+      int c[n], any = 0;
+      float y[n];
+#pragma unroll
+      for (int e = 0; e < n; e += 4) {
+        int4* four = reinterpret_cast<int4*>(&count[at + e]);
+        c[e] = four->x, c[e + 1] = four->y, c[e + 2] = four->z, c[e + 3] = four->w;
+        any |= four->x | four->y | four->z | four->w;
+      }
+#pragma unroll
+      for (int e = 0; e < n; ++e) y[e] = to_float(now[k].v[e]);
+      if (any) {
+#pragma unroll
+        for (int e = 0; e < n; e += 4) *reinterpret_cast<int4*>(&count[at + e]) = int4{0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < n; ++e)
+          if (c[e]) y[e] = (y[e] > 0 ? y[e] / rep : y[e] * rep) - (pres + freq * static_cast<float>(c[e]));
+      }
+      if (BIAS)
+#pragma unroll
+        for (int e = 0; e < n; e += 4) {
+          float4* four = reinterpret_cast<float4*>(&bias[at + e]);
+          y[e] += four->x, y[e + 1] += four->y, y[e + 2] += four->z, y[e + 3] += four->w;
+          *four = float4{0, 0, 0, 0};
+        }
+      if (allowed) {
+        const int v0 = v < 0 ? 0 : v, word = v0 >> 5, v1 = v + n - 1 < a.cols ? v + n - 1 : a.cols - 1;
+        const uint64_t bits = (static_cast<uint64_t>(allowed[v1 >> 5]) << ((v1 >> 5) == word ? 0 : 32) | allowed[word]) >> (v0 & 31);
+#pragma unroll
+        for (int e = 0; e < n; ++e) {
+          const int b = v + e - v0;
+          if (b >= 0 && !(bits >> b & 1)) y[e] = -INFINITY;
+        }
+      }
+      Values<T> z;
+#pragma unroll
+      for (int e = 0; e < n; ++e) z.v[e] = from_float<T>(y[e]);
+      if (aligned && v >= 0 && v + n <= a.cols) {
+        *reinterpret_cast<Values<T>*>(__builtin_assume_aligned(out + v, 16)) = z;
+      } else {
+#pragma unroll
+        for (int e = 0; e < n; ++e)
+          if (v + e >= 0 && v + e < a.cols) out[v + e] = z.v[e];
+      }
+    }
+    if (!more) return;
+    lo = static_cast<int>(following);
+    lds_barrier();
+  }
+}
+
+template <class T, int VECS>
+void launch(const Logits& a, int most, hipStream_t stream) {
+  constexpr int segment = kThreads * VECS * Vec16<T>::n;
+  // a row that begins in the middle of 16 bytes has up to 15 bytes more
+  const int64_t segments = (static_cast<int64_t>(a.cols) + Vec16<T>::n - 1 + segment - 1) / segment;
+  const int64_t parts = a.rows < most ? most / a.rows : 1;
+  const dim3 grid(a.rows, static_cast<unsigned>(parts < segments ? parts : segments));
+  if (a.bias.pos) logits_kernel<T, VECS, true><<<grid, kThreads, 0, stream>>>(a);
+  else logits_kernel<T, VECS, false><<<grid, kThreads, 0, stream>>>(a);
+}
+
+template <class T>
+void dispatch(const Logits& a, hipStream_t stream) {
+  launch<T, 1>(a, 1024, stream);
 }
 
 }  // namespace
@@ -77,10 +195,9 @@ spt_status adjust_logits_dispatch(int32_t dtype, int64_t R, int64_t V, const voi
                  static_cast<int>(rules->sequences), rules->first, pattern_view(rules->seen), pattern_view(rules->tree),
                  pattern_view(rules->bias), rules->bias ? static_cast<const float*>(rules->bias->vals) : nullptr, rules->drafts,
                  rules->repetition, rules->presence, rules->frequency, rules->allowed};
-  const dim3 grid(static_cast<unsigned>(R), static_cast<unsigned>((V + kSegment - 1) / kSegment));
-  if (dtype == SPT_F32) logits_kernel<float><<<grid, kBlock, 0, stream>>>(a);
-  else if (dtype == SPT_F16) logits_kernel<f16><<<grid, kBlock, 0, stream>>>(a);
-  else logits_kernel<bf16><<<grid, kBlock, 0, stream>>>(a);
+  if (dtype == SPT_F32) dispatch<float>(a, stream);
+  else if (dtype == SPT_F16) dispatch<f16>(a, stream);
+  else dispatch<bf16>(a, stream);
   SPT_CHECK_LAUNCH("adjust_logits");
   return SPT_OK;
 }
