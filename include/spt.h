@@ -458,7 +458,7 @@ spt_status spt_validate(const spt_tensor* T, int32_t* err_dev, void* stream);
  *
  *   dtype      SPT_F32, SPT_F16 or SPT_BF16; of K, V and of every k, v, q and out below
  *   layers     >= 1; the layers share table, len and refs
- *   heads      >= 1, of K and V
+ *   heads      >= 1, of K and V; layers * heads <= 65536
  *   width      values of a head: a multiple of 8, 8 .. 256
  *   page       slots of a page: a power of two, 1 .. 65536
  *   rows       <= 2^20; row_pages: places of a row of the table

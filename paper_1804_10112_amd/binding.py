@@ -171,7 +171,7 @@ def _p(t):
 
 
 def _desc(T):
-    return C.addressof(T.c) if isinstance(T, (DeviceTensor, DeviceCSR, DeviceCache, LogitRules)) else C.addressof(T)
+    return C.addressof(T.c) if isinstance(T, (DeviceTensor, DeviceCSR)) else C.addressof(T)
 
 
 _raw_stream = _device = None
@@ -409,20 +409,33 @@ def _invalid(message):
     raise SptError(SPT_ERR_INVALID_ARG, message)
 
 
+_codes = {}
+
+
 def _dtype_code(dtype):
-    import torch
-    codes = {torch.float32: SPT_F32, torch.float64: SPT_F64, torch.float16: SPT_F16, torch.bfloat16: SPT_BF16}
-    if dtype not in codes:
+    if not _codes:
+        import torch
+        _codes.update({torch.float32: SPT_F32, torch.float64: SPT_F64, torch.float16: SPT_F16, torch.bfloat16: SPT_BF16})
+    if dtype not in _codes:
         raise TypeError(f"values must be float32, float16 or bfloat16, got {dtype}")
-    return codes[dtype]
+    return _codes[dtype]
+
+
+_int32 = None   # torch.int32, once a descriptor has imported torch: an import statement in a call costs a tenth of it
+
+
+def _use_torch():
+    global _int32
+    import torch
+    _int32 = torch.int32
+    return torch
 
 
 def _i32(t, count, name):
     """Device pointer of a contiguous int32 tensor of at least `count` entries (None -> NULL)."""
-    import torch
     if t is None:
         return None
-    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < count:
+    if t.dtype is not _int32 or t.numel() < count or not t.is_contiguous():
         _invalid(f"{name} must be a contiguous int32 tensor of at least {count} entries")
     return t.data_ptr()
 
@@ -437,6 +450,7 @@ class DeviceCSR:
     vals float32 or float64; without vals a pattern."""
 
     def __init__(self, pos, crd, cols, vals=None, ordered=False, unique=False):
+        _use_torch()
         rows = pos.numel() - 1
         t = SptTensor()
         t.order = t.nlevels = 2
@@ -458,7 +472,7 @@ class DeviceCache:
     contiguous values of a head, table (rows, pages of a row), len (rows) and refs (pages), int32 and contiguous."""
 
     def __init__(self, K, V, table, length, refs):
-        import torch
+        _use_torch()
         if K.dim() != 5 or K.shape != V.shape or K.stride() != V.stride() or K.dtype != V.dtype:
             _invalid("K and V must be alike: (layers, pages, slots of a page, heads, width)")
         if K.stride(4) != 1:
@@ -473,7 +487,8 @@ class DeviceCache:
         c.K, c.V = K.data_ptr(), V.data_ptr()
         c.table, c.len, c.refs = _i32(table, 0, "table"), _i32(length, c.rows, "len"), _i32(refs, c.pages, "refs")
         self.K, self.V, self.table, self.len, self.refs = K, V, table, length, refs
-        self.c = c
+        self.c, self.address = c, C.addressof(c)
+        self.rows, self.heads, self.width, self.dtype = c.rows, c.heads, c.width, K.dtype
 
     def workspace(self, op, q_heads=0):
         import torch
@@ -481,13 +496,14 @@ class DeviceCache:
 
     def _tokens(self, t, name, heads):
         """(tokens, heads, width) of the cache's dtype: token and head strides."""
-        if t.dtype != self.K.dtype or t.dim() != 3 or t.shape[2] != self.c.width or t.shape[1] != heads or t.stride(2) != 1:
-            _invalid(f"{name} must be (tokens, {heads}, {self.c.width}), {self.K.dtype}, values of a head contiguous")
-        return _stride(t, 0), _stride(t, 1)
+        shape, stride = t.shape, t.stride()
+        if t.dtype is not self.dtype or len(shape) != 3 or shape[2] != self.width or shape[1] != heads or stride[2] != 1:
+            _invalid(f"{name} must be (tokens, {heads}, {self.width}), {self.dtype}, values of a head contiguous")
+        return (stride[0] if shape[0] > 1 else 0), (stride[1] if heads > 1 else 0)
 
 
 def spt_cache_workspace_bytes(op, cache, q_heads=0) -> int:
-    n = lib().spt_cache_workspace_bytes(op, _desc(cache), q_heads)
+    n = lib().spt_cache_workspace_bytes(op, cache.address, q_heads)
     if n == 0:
         raise SptError(SPT_ERR_INVALID_ARG, spt_last_error())
     return n
@@ -495,44 +511,46 @@ def spt_cache_workspace_bytes(op, cache, q_heads=0) -> int:
 
 def spt_cache_extend(cache, add, refused_dev, ws=None, stream=None):
     p, n = _ws(ws)
-    _check(lib().spt_cache_extend(_desc(cache), _i32(add, cache.c.rows, "add"), _i32(refused_dev, 1, "refused_dev"), p, n,
+    _check(lib().spt_cache_extend(cache.address, _i32(add, cache.rows, "add"), _i32(refused_dev, 1, "refused_dev"), p, n,
                                   _stream(stream)))
 
 
 def spt_cache_write(cache, layer, first, k, v, stream=None):
-    token, head = cache._tokens(k, "k", cache.c.heads)
-    if k.shape[0] != v.shape[0] or cache._tokens(v, "v", cache.c.heads) != (token, head):
+    token, head = cache._tokens(k, "k", cache.heads)
+    tokens = k.shape[0]
+    if cache._tokens(v, "v", cache.heads) != (token, head) or v.shape[0] != tokens:
         _invalid("k and v must be alike")
-    _check(lib().spt_cache_write(_desc(cache), layer, _i32(first, cache.c.rows + 1, "first"), k.shape[0], _p(k), _p(v), token, head,
-                                 _stream(stream)))
+    _check(lib().spt_cache_write(cache.address, layer, _i32(first, cache.rows + 1, "first"), tokens, k.data_ptr(), v.data_ptr(), token,
+                                 head, _stream(stream)))
 
 
 def spt_cache_compact(cache, first, keep, stream=None):
-    _check(lib().spt_cache_compact(_desc(cache), _i32(first, cache.c.rows + 1, "first"), keep and _desc(keep), _stream(stream)))
+    _check(lib().spt_cache_compact(cache.address, _i32(first, cache.rows + 1, "first"), keep and _desc(keep), _stream(stream)))
 
 
 def spt_cache_free(cache, new_len, stream=None):
-    _check(lib().spt_cache_free(_desc(cache), _i32(new_len, cache.c.rows, "new_len"), _stream(stream)))
+    _check(lib().spt_cache_free(cache.address, _i32(new_len, cache.rows, "new_len"), _stream(stream)))
 
 
 def spt_cache_fork(cache, parents, children, stream=None):
     n = children.numel()
-    _check(lib().spt_cache_fork(_desc(cache), n, _i32(parents, n, "parents"), _i32(children, n, "children"), _stream(stream)))
+    _check(lib().spt_cache_fork(cache.address, n, _i32(parents, n, "parents"), _i32(children, n, "children"), _stream(stream)))
 
 
 def spt_cache_attention(cache, layer, first, tree, q, scale, out, lse=None, ws=None, stream=None):
     """q, out: (tokens, q_heads, width); tree: DeviceCSR or None; lse: float32 (tokens, q_heads), contiguous, or None."""
-    import torch
-    heads = q.shape[1] if q.dim() == 3 else 0
+    shape = q.shape
+    heads = shape[1] if len(shape) == 3 else 0
     q_token, q_head = cache._tokens(q, "q", heads)
     out_token, out_head = cache._tokens(out, "out", heads)
-    if out.shape[0] != q.shape[0]:
+    if out.shape != shape:
         _invalid("q and out have different numbers of tokens")
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous()):
+    if lse is not None and (lse.shape != shape[:2] or lse.element_size() != 4 or not lse.is_floating_point()
+                            or not lse.is_contiguous()):
         _invalid("lse must be float32, (tokens, q_heads), contiguous")
     p, n = _ws(ws)
-    _check(lib().spt_cache_attention(_desc(cache), layer, _i32(first, cache.c.rows + 1, "first"), q.shape[0], tree and _desc(tree),
-                                     _p(q), heads, q_token, q_head, scale, _p(out), out_token, out_head, _p(lse), p, n,
+    _check(lib().spt_cache_attention(cache.address, layer, _i32(first, cache.rows + 1, "first"), shape[0], tree and _desc(tree),
+                                     q.data_ptr(), heads, q_token, q_head, scale, out.data_ptr(), out_token, out_head, _p(lse), p, n,
                                      _stream(stream)))
 
 
@@ -542,7 +560,7 @@ class LogitRules:
 
     def __init__(self, first=None, seen=None, tree=None, drafts=None, repetition=None, presence=None, frequency=None, bias=None,
                  allowed=None, sequences=None):
-        import torch
+        torch = _use_torch()
         per_sequence = [t for t in (repetition, presence, frequency) if t is not None]
         if sequences is None:
             counts = ([first.numel() - 1] if first is not None else []) + [m.c.level[0].N for m in (seen, bias) if m is not None]
@@ -565,16 +583,21 @@ class LogitRules:
             r.allowed, r.allowed_stride = allowed.data_ptr(), max(_stride(allowed, 0), allowed.shape[1])
         self.keep = (first, seen, tree, drafts, repetition, presence, frequency, bias, allowed)
         self.rows = min([t.shape[0] for t in (drafts, allowed) if t is not None], default=None)
-        self.c = r
+        self.c, self.address = r, C.addressof(r)
 
 
 def spt_adjust_logits(logits, rules, out, stream=None):
     """logits, out: (rows, vocabulary) of one dtype, values of a row contiguous; they may be the same tensor."""
-    if logits.dim() != 2 or logits.shape != out.shape or logits.dtype != out.dtype or _stride(logits, 1) > 1 or _stride(out, 1) > 1:
-        _invalid("logits and out must be alike: (rows, vocabulary), values of a row contiguous")
-    if rules.rows is not None and rules.rows < logits.shape[0]:
+    shape, dtype = logits.shape, logits.dtype
+    if len(shape) != 2 or out.shape != shape or out.dtype is not dtype:
+        _invalid("logits and out must be alike: (rows, vocabulary)")
+    R, V = shape
+    (stride, inner), (out_stride, out_inner) = logits.stride(), out.stride()
+    if V > 1 and (inner != 1 or out_inner != 1):
+        _invalid("the values of a row of logits and out must be contiguous")
+    if R <= 1:
+        stride = out_stride = V
+    if rules.rows is not None and rules.rows < R:
         _invalid("drafts or allowed have fewer rows than logits")
-    R, V = logits.shape
-    stride, out_stride = (_stride(t, 0) if R > 1 else V for t in (logits, out))
-    _check(lib().spt_adjust_logits(_dtype_code(logits.dtype), R, V, _p(logits), stride, _desc(rules), _p(out), out_stride,
+    _check(lib().spt_adjust_logits(_dtype_code(dtype), R, V, logits.data_ptr(), stride, rules.address, out.data_ptr(), out_stride,
                                    _stream(stream)))

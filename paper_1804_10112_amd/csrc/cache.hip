@@ -51,9 +51,10 @@ __global__ void fork_kernel(Cache c, int n, const int32_t* __restrict__ parents,
 
 // ---- extend -----------------------------------------------------------------------------------------------------------------
 //
-// Three launches. (1) Workgroups count the free pages of a stretch of the pool each; one more goes through the rows and writes
-// the running sum of the pages they want. (2) With both, the k-th free page finds the row and the place it goes to. (3) Copies
-// on write, lengths, and the shared pages' refs, which (1) and (2) both have to find as they were.
+// Three steps. (1) The free pages are counted, in stretches of the pool, and the rows are gone through for the running sum of the
+// pages they want. (2) With both, the k-th free page finds the row and the place it goes to. (3) Copies on write, lengths, and the
+// shared pages' refs, which (1) and (2) both have to find as they were. A launch each; the first two are one workgroup's where its
+// threads hold the whole pool's refs in registers.
 
 struct Wanted {
   int start, count;  // places start .. start+count-1 of the table
@@ -93,28 +94,19 @@ struct Plan {
   int32_t* total;       // free pages in all
 };
 
-__global__ void __launch_bounds__(kScanBlock) extend_count_kernel(Cache c, const int32_t* __restrict__ add, int stretch, Plan plan,
-                                                                  int32_t* refused) {
-  __shared__ int lds[kScanBlock / kWave];
-  if (blockIdx.x + 1 < gridDim.x) {
-    const int lo = blockIdx.x * stretch, hi = c.pages - lo < stretch ? c.pages : lo + stretch;
-    int n = 0;
-    for (int p = lo + threadIdx.x; p < hi; p += kScanBlock) n += c.refs[p] == 0;
-    n = block_inclusive_scan(n, lds);
-    if (threadIdx.x == kScanBlock - 1) plan.free_pages[blockIdx.x] = n;
-    return;
-  }
+// Step (1) of the rows, by a whole workgroup.
+__device__ __forceinline__ void want(const Cache& c, const int32_t* __restrict__ add, const Plan& plan, int32_t* refused, int* lds) {
   int before = 0;
   for (int base = 0; base < c.rows; base += kScanBlock) {
     const int s = base + threadIdx.x;
     int n = 0, from = -1;
     if (s < c.rows) {
-      const int length = row_length(c, s);
-      if (add[s] > 0 && (length & ((1 << c.shift) - 1)) != 0) {
+      const int length = row_length(c, s), more = add[s];
+      if (more > 0 && (length & ((1 << c.shift) - 1)) != 0) {
         const int p = page_at(c, s, length >> c.shift);
         if (p >= 0 && c.refs[p] > 1) from = p;
       }
-      n = wanted(c, length, add[s], from >= 0).count;
+      n = wanted(c, length, more, from >= 0).count;
       plan.copied[s] = from;
       plan.fill[s] = length & ((1 << c.shift) - 1);
     }
@@ -126,6 +118,77 @@ __global__ void __launch_bounds__(kScanBlock) extend_count_kernel(Cache c, const
     before = lds[0];
   }
   if (threadIdx.x == 0) *refused = 0;
+}
+
+// Step (2) of free page p, the k-th of `total`.
+__device__ __forceinline__ void assign(const Cache& c, const int32_t* __restrict__ add, const Plan& plan, int p, int k, int total) {
+  int s = 0, n = c.rows;  // the first row with end > k
+  while (n > 0) {
+    const int half = n >> 1;
+    if (plan.end[s + half] <= k) s += half + 1, n -= half + 1;
+    else n = half;
+  }
+  if (plan.end[s] > total) return;
+  const Wanted w = wanted(c, row_length(c, s), add[s], plan.copied[s] >= 0);
+  const int place = k - (plan.end[s] - w.count);
+  c.table[static_cast<int64_t>(s) * c.row_pages + w.start + place] = p;
+  c.refs[p] = 1;
+  if (place == 0) plan.target[s] = p;
+}
+
+constexpr int kHeld = 16;  // refs that a thread holds of a small pool
+
+__global__ void __launch_bounds__(kScanBlock) extend_small_kernel(Cache c, const int32_t* __restrict__ add, Plan plan,
+                                                                  int32_t* refused) {
+  __shared__ int lds[kScanBlock / kWave];
+  // bit k: page k * kScanBlock + thread is free; pages in ascending order are ranked group by group
+  uint32_t is_free = 0;
+  int held[kHeld];
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) {
+    const int p = k * kScanBlock + threadIdx.x;
+    held[k] = p < c.pages ? c.refs[p] : 1;
+  }
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) is_free |= (held[k] == 0) << k;
+  want(c, add, plan, refused, lds);
+  __shared__ int in_wave[kHeld][kScanBlock / kWave];  // free pages of each group and wave, then of all before them
+  __shared__ int sum;
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) {
+    const int n = __popcll(__ballot(is_free >> k & 1));
+    if (lane_id() == 0) in_wave[k][wave_id()] = n;
+  }
+  __syncthreads();
+  constexpr int kCounts = kHeld * (kScanBlock / kWave);
+  static_assert(kCounts <= kScanBlock, "a count a thread");
+  const int mine = threadIdx.x < kCounts ? (&in_wave[0][0])[threadIdx.x] : 0, upto = block_inclusive_scan(mine, lds);
+  __syncthreads();
+  if (threadIdx.x < kCounts) (&in_wave[0][0])[threadIdx.x] = upto - mine;
+  if (threadIdx.x == kScanBlock - 1) sum = upto;
+  __syncthreads();
+  const int total = sum, needed = c.rows ? plan.end[c.rows - 1] : 0;
+  if (threadIdx.x == 0) *plan.total = total;
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) {
+    const uint64_t b = __ballot(is_free >> k & 1);
+    const int rank = in_wave[k][wave_id()] + __popcll(b & ((uint64_t(1) << lane_id()) - 1));
+    if ((is_free >> k & 1) && rank < needed) assign(c, add, plan, k * kScanBlock + threadIdx.x, rank, total);
+  }
+}
+
+__global__ void __launch_bounds__(kScanBlock) extend_count_kernel(Cache c, const int32_t* __restrict__ add, int stretch, Plan plan,
+                                                                  int32_t* refused) {
+  __shared__ int lds[kScanBlock / kWave];
+  if (blockIdx.x + 1 == gridDim.x) {
+    want(c, add, plan, refused, lds);
+    return;
+  }
+  const int lo = blockIdx.x * stretch, hi = c.pages - lo < stretch ? c.pages : lo + stretch;
+  int n = 0;
+  for (int p = lo + threadIdx.x; p < hi; p += kScanBlock) n += c.refs[p] == 0;
+  n = block_inclusive_scan(n, lds);
+  if (threadIdx.x == kScanBlock - 1) plan.free_pages[blockIdx.x] = n;
 }
 
 __global__ void __launch_bounds__(kScanBlock) extend_assign_kernel(Cache c, const int32_t* __restrict__ add, int stretch, Plan plan) {
@@ -150,22 +213,8 @@ __global__ void __launch_bounds__(kScanBlock) extend_assign_kernel(Cache c, cons
   for (int base = lo; base < hi && rank < needed; base += kScanBlock) {
     const int p = base + threadIdx.x;
     const int is_free = p < hi && c.refs[p] == 0;
-    const int upto = rank + block_inclusive_scan(is_free, lds), k = upto - 1;
-    if (is_free && k < needed) {
-      int s = 0, n = c.rows;  // the first row with end > k
-      while (n > 0) {
-        const int half = n >> 1;
-        if (plan.end[s + half] <= k) s += half + 1, n -= half + 1;
-        else n = half;
-      }
-      if (plan.end[s] <= total) {
-        const Wanted w = wanted(c, row_length(c, s), add[s], plan.copied[s] >= 0);
-        const int place = k - (plan.end[s] - w.count);
-        c.table[static_cast<int64_t>(s) * c.row_pages + w.start + place] = p;
-        c.refs[p] = 1;
-        if (place == 0) plan.target[s] = p;
-      }
-    }
+    const int upto = rank + block_inclusive_scan(is_free, lds);
+    if (is_free && upto <= needed) assign(c, add, plan, p, upto - 1, total);
     __syncthreads();
     if (threadIdx.x == kScanBlock - 1) lds[0] = upto;
     __syncthreads();
@@ -239,28 +288,50 @@ __device__ __forceinline__ int kept(const Cache& c, const Pattern& keep, int s, 
   return clamped(pattern_end(keep, s) - pattern_begin(keep, s), 0, drafts);
 }
 
-// A thread owns 16 bytes of each token of the row (in one layer, K or V, and head) and moves them token after token: the kept ones
-// ascend, so a slot that is written was read before and is not read again.
-__global__ void compact_move_kernel(Cache c, const int32_t* __restrict__ first, Pattern keep) {
+// A thread owns 16 bytes of each token of the row (in one layer, K or V, and head) and moves them token after token, kBatch loads at a
+// time: the kept ones ascend, so a slot that is written was read before and is not read again. Where the tokens lie the workgroup
+// finds out first, kMoves of them at a time.
+constexpr int kMoves = kBlock, kBatch = 8;
+typedef int Bytes16 __attribute__((ext_vector_type(4)));
+__global__ void __launch_bounds__(kBlock) compact_move_kernel(Cache c, const int32_t* __restrict__ first, Pattern keep) {
+  __shared__ int64_t from[kMoves], to[kMoves];  // -1: stays where it is
   const int s = blockIdx.x, vecs = c.width_bytes / 16;
-  int64_t r = blockIdx.y * static_cast<int64_t>(blockDim.x) + threadIdx.x;
-  if (r >= static_cast<int64_t>(c.layers) * 2 * c.heads * vecs) return;
+  const Drafted d = drafted(first, s, INT32_MAX);
+  const int context = row_length(c, s) - d.count, begin = pattern_begin(keep, s), n = kept(c, keep, s, d.count);
+  if (context < 0 || n == 0) return;
+  int r = blockIdx.y * blockDim.x + threadIdx.x;
+  const bool mine = r < c.layers * 2 * c.heads * vecs;
   const int v = r % vecs;
   r /= vecs;
   const int h = r % c.heads;
   r /= c.heads;
   char* pool = ((r & 1) ? c.V : c.K) + (r >> 1) * c.layer_bytes + h * c.head_bytes + v * 16;
-  const Drafted d = drafted(first, s, INT32_MAX);
-  const int context = row_length(c, s) - d.count, begin = pattern_begin(keep, s), n = kept(c, keep, s, d.count);
-  if (context < 0) return;
-  for (int j = 0; j < n; ++j) {
-    const int from = keep.crd[begin + j];
-    if (from <= j || from >= d.count) continue;
-    const int a = context + from, b = context + j, pa = page_at(c, s, a >> c.shift), pb = page_at(c, s, b >> c.shift);
-    if (pa < 0 || pb < 0) continue;
-    const int mask = (1 << c.shift) - 1;
-    *reinterpret_cast<int4*>(pool + pb * c.page_bytes + (b & mask) * c.slot_bytes) =
-        *reinterpret_cast<const int4*>(pool + pa * c.page_bytes + (a & mask) * c.slot_bytes);
+  for (int base = 0; base < n; base += kMoves) {
+    __syncthreads();
+    const int j = base + threadIdx.x;
+    if (j < n) {
+      const int f = keep.crd[begin + j];
+      int64_t a = -1, b = -1;
+      if (f > j && f < d.count) {
+        const int x = context + f, y = context + j, px = page_at(c, s, x >> c.shift), py = page_at(c, s, y >> c.shift);
+        const int mask = (1 << c.shift) - 1;
+        if (px >= 0 && py >= 0) a = px * c.page_bytes + (x & mask) * c.slot_bytes, b = py * c.page_bytes + (y & mask) * c.slot_bytes;
+      }
+      from[threadIdx.x] = a;
+      to[threadIdx.x] = b;
+    }
+    __syncthreads();
+    const int count = n - base < kMoves ? n - base : kMoves;
+    if (mine)
+      for (int k = 0; k < count; k += kBatch) {
+        Bytes16 x[kBatch];
+#pragma unroll
+        for (int e = 0; e < kBatch; ++e)
+          if (k + e < count && from[k + e] >= 0) x[e] = *reinterpret_cast<const Bytes16*>(pool + from[k + e]);
+#pragma unroll
+        for (int e = 0; e < kBatch; ++e)
+          if (k + e < count && from[k + e] >= 0) *reinterpret_cast<Bytes16*>(pool + to[k + e]) = x[e];
+      }
   }
 }
 
@@ -296,13 +367,17 @@ spt_status cache_extend_dispatch(const spt_cache* cache, const int32_t* add, int
   plan.target = w.take<int32_t>(c.rows);
   plan.fill = w.take<int32_t>(c.rows);
   plan.total = w.take<int32_t>(1);
-  const int stretch = stretch_of(c.pages), blocks = c.pages ? (c.pages + stretch - 1) / stretch : 1;
-  extend_count_kernel<<<blocks + 1, kScanBlock, 0, stream>>>(c, add, stretch, plan, refused);
+  if (c.pages <= kHeld * kScanBlock) {
+    extend_small_kernel<<<1, kScanBlock, 0, stream>>>(c, add, plan, refused);
+  } else {
+    const int stretch = stretch_of(c.pages), blocks = (c.pages + stretch - 1) / stretch;
+    extend_count_kernel<<<blocks + 1, kScanBlock, 0, stream>>>(c, add, stretch, plan, refused);
+    if (c.rows > 0) extend_assign_kernel<<<blocks, kScanBlock, 0, stream>>>(c, add, stretch, plan);
+  }
   if (c.rows == 0) {
     SPT_CHECK_LAUNCH("cache_extend");
     return SPT_OK;
   }
-  extend_assign_kernel<<<blocks, kScanBlock, 0, stream>>>(c, add, stretch, plan);
   const int64_t units = static_cast<int64_t>(c.layers) * 2 * c.heads * (c.width_bytes / 16) << c.shift;
   int64_t y = (units + 8 * kBlock - 1) / (8 * kBlock);
   const int64_t most = c.rows < 8192 ? 8192 / c.rows : 1;

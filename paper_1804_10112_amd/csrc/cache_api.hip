@@ -50,6 +50,8 @@ static spt_status cache_ok(const spt_cache* c, const char* what) {
     return fail(SPT_ERR_UNSUPPORTED, "%s: width %d is not a multiple of 8 from 8 to 256", what, c->width);
   if (c->page < 1 || c->page > 65536 || (c->page & (c->page - 1)) != 0)
     return fail(SPT_ERR_UNSUPPORTED, "%s: page %d is not a power of two from 1 to 65536", what, c->page);
+  if (static_cast<int64_t>(c->layers) * c->heads > 65536)
+    return fail(SPT_ERR_UNSUPPORTED, "%s: %d layers of %d heads, at most 65536 in all", what, c->layers, c->heads);
   if (c->rows < 0 || c->row_pages < 0 || c->pages < 0 || c->pages >= INT32_MAX)
     return fail(SPT_ERR_INVALID_ARG, "%s: rows, row_pages or pages out of range", what);
   if (c->rows > kMaxRows) return fail(SPT_ERR_UNSUPPORTED, "%s: %d rows, at most %lld", what, c->rows, (long long)kMaxRows);
