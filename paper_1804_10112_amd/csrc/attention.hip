@@ -213,54 +213,114 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
 }
 
 // Joins the parts of tiles that lie in several workgroups. blockIdx.x is a workgroup that began within a tile; those of one tile share
-// its rows, and blockIdx.y divides them further. Few parts: a wave takes a row; many: the waves of a workgroup share the parts of it.
+// its rows, and blockIdx.y divides them further. Few parts: 16 lanes take a row, and all their loads are under way at once; many: the
+// waves of a workgroup share the parts of a row.
 constexpr int kFewParts = 8;
 template <class T, int WIDTH, int ROWS>
 __global__ void __launch_bounds__(kBlock) attention_join_kernel(Attention a) {
-  constexpr int kEach = WIDTH / kWave;  // values of a lane
+  constexpr int kEach = WIDTH / 16;  // values of a lane
   __shared__ float area[kWaves][WIDTH], sums[kWaves];
   const Part part = a.part[blockIdx.x];
   if (part.parts == 0) return;
   const Drafted d = drafted(a.first, part.s, a.total);
   const int left = d.count * a.group - part.row, rows = left < ROWS ? left : ROWS;
-  const int lane = lane_id(), wave = wave_id(), width = a.c.width_bytes / static_cast<int>(sizeof(T));
+  const int lane = lane_id(), wave = wave_id(), i = lane & 15, quad = lane >> 4;
   constexpr int64_t kSlot = static_cast<int64_t>(ROWS) * (WIDTH + 2);
   const float* second = a.partial + (static_cast<int64_t>(blockIdx.x) - part.place) * 2 * kSlot;  // part p > 0: slot 0 of p - 1 groups on
   auto slot = [&](int p) { return p ? second + (p - 1) * 2 * kSlot : second - kSlot; };
-  const bool many = part.parts > kFewParts;
   const int takers = (part.parts - 1) * gridDim.y, taker = part.place * gridDim.y + blockIdx.y;
-  for (int r = many ? taker : taker * kWaves + wave; r < rows; r += many ? takers : takers * kWaves) {
-    float top = -INFINITY, sum = 0, y[kEach] = {};
+
+  // The lane's values 4 i + 64 e .. of row r: those of part p, weighed.
+  auto add = [&](int p, int r, float zero, float& sum, f4(&y)[kEach / 4]) {
+    const float* from = slot(p);
+    const float f = exp2_of(from[r] - zero);
+    sum += f * from[ROWS + r];
+#pragma unroll
+    for (int e = 0; e < kEach / 4; ++e) y[e] += f * *reinterpret_cast<const f4*>(from + 2 * ROWS + r * WIDTH + 64 * e + 4 * i);
+  };
+  auto write = [&](int r, float top, float sum, const f4(&y)[kEach / 4]) {
+    const int row = part.row + r, token = d.begin + row / a.by_group, h = part.head * a.group + row - (token - d.begin) * a.group;
+    T* to = reinterpret_cast<T*>(a.out + token * a.out_token_bytes + h * a.out_head_bytes);
+    const int width = a.c.width_bytes / static_cast<int>(sizeof(T));
+#pragma unroll
+    for (int e = 0; e < kEach / 4; ++e)
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        if (64 * e + 4 * i < width) to[64 * e + 4 * i + b] = from_float<T>(sum == 0 ? 0.0f : y[e][b] / sum);
+    if (i == 0 && a.lse) a.lse[static_cast<int64_t>(token) * a.q_heads + h] = natural_lse(top, sum);
+  };
+
+  if (part.parts <= kFewParts) {
+    for (int r = (taker * kWaves + wave) * 4 + quad; r < rows; r += takers * kWaves * 4) {
+      float top = -INFINITY, sum = 0;
+      f4 y[kEach / 4] = {};
+      float m[kFewParts], l[kFewParts];
+      f4 x[kFewParts / 2][kEach / 4];
+      auto load = [&](int p0) {  // of four parts, again the last one where there are fewer
+#pragma unroll
+        for (int p = 0; p < kFewParts / 2; ++p) {
+          const float* from = slot(p0 + p < part.parts ? p0 + p : part.parts - 1);
+          m[p0 + p] = from[r];
+          l[p0 + p] = from[ROWS + r];
+#pragma unroll
+          for (int e = 0; e < kEach / 4; ++e) x[p][e] = *reinterpret_cast<const f4*>(from + 2 * ROWS + r * WIDTH + 64 * e + 4 * i);
+        }
+      };
+      auto add_loaded = [&](int p0, float rescale) {
+        const float zero = top == -INFINITY ? 0 : top;
+        sum *= rescale;
+#pragma unroll
+        for (int e = 0; e < kEach / 4; ++e) y[e] *= rescale;
+#pragma unroll
+        for (int p = 0; p < kFewParts / 2; ++p) {
+          if (p0 + p >= part.parts) continue;
+          const float f = exp2_of(m[p0 + p] - zero);
+          sum += f * l[p0 + p];
+#pragma unroll
+          for (int e = 0; e < kEach / 4; ++e) y[e] += f * x[p][e];
+        }
+      };
+      load(0);
+#pragma unroll
+      for (int p = 0; p < kFewParts / 2; ++p) top = fmaxf(top, m[p]);
+      add_loaded(0, 1);
+      if (part.parts > kFewParts / 2) {
+        load(kFewParts / 2);
+        const float before = top;
+#pragma unroll
+        for (int p = kFewParts / 2; p < kFewParts; ++p) top = fmaxf(top, m[p]);
+        add_loaded(kFewParts / 2, exp2_of(before - (top == -INFINITY ? 0 : top)));
+      }
+      write(r, top, sum, y);
+    }
+    return;
+  }
+  for (int r = taker; r < rows; r += takers) {  // the 16 lanes of each quad take every fourth of the wave's parts
+    float top = -INFINITY, sum = 0;
+    f4 y[kEach / 4] = {};
     for (int p = lane; p < part.parts; p += kWave) top = fmaxf(top, slot(p)[r]);
     for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
     const float zero = top == -INFINITY ? 0 : top;
 #pragma unroll 4
-    for (int p = many ? wave : 0; p < part.parts; p += many ? kWaves : 1) {
-      const float* from = slot(p);
-      const float f = exp2_of(from[r] - zero);
-      sum += f * from[ROWS + r];
+    for (int p = wave * 4 + quad; p < part.parts; p += kWaves * 4) add(p, r, zero, sum, y);
+    sum = sum_of_row(sum);
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) y[e] += f * from[2 * ROWS + r * WIDTH + lane * kEach + e];
+    for (int e = 0; e < kEach / 4; ++e)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) y[e][b] = sum_of_row(y[e][b]);
+    __syncthreads();
+    if (quad == 0)
+#pragma unroll
+      for (int e = 0; e < kEach / 4; ++e) *reinterpret_cast<f4*>(&area[wave][64 * e + 4 * i]) = y[e];
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    if (wave != 0 || quad != 0) continue;
+    for (int w = 1; w < kWaves; ++w) {
+      sum += sums[w];
+#pragma unroll
+      for (int e = 0; e < kEach / 4; ++e) y[e] += *reinterpret_cast<const f4*>(&area[w][64 * e + 4 * i]);
     }
-    if (many) {
-      __syncthreads();
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) area[wave][lane * kEach + e] = y[e];
-      if (lane == 0) sums[wave] = sum;
-      __syncthreads();
-      if (wave != 0) continue;
-      for (int w = 1; w < kWaves; ++w) {
-        sum += sums[w];
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) y[e] += area[w][lane * kEach + e];
-      }
-    }
-    const int row = part.row + r, token = d.begin + row / a.by_group, h = part.head * a.group + row - (token - d.begin) * a.group;
-    T* to = reinterpret_cast<T*>(a.out + token * a.out_token_bytes + h * a.out_head_bytes);
-#pragma unroll
-    for (int e = 0; e < kEach; ++e)
-      if (lane * kEach + e < width) to[lane * kEach + e] = from_float<T>(sum == 0 ? 0.0f : y[e] / sum);
-    if (lane == 0 && a.lse) a.lse[static_cast<int64_t>(token) * a.q_heads + h] = natural_lse(top, sum);
+    write(r, top, sum, y);
   }
 }
 
@@ -286,7 +346,7 @@ void launch_few_rows(const Attention& a, hipStream_t stream) {
 
 template <class T, int WIDTH>
 void launch_join_width(const Attention& a, int groups, int rows, hipStream_t stream) {
-  const dim3 grid(groups, rows / 16);  // of a tile of two parts, four rows to a wave
+  const dim3 grid(groups, rows / 16);  // a tile of two parts: four rows to each wave
   if (rows == 16) attention_join_kernel<T, WIDTH, 16><<<grid, kBlock, 0, stream>>>(a);
   else if (rows == 32) attention_join_kernel<T, WIDTH, 32><<<grid, kBlock, 0, stream>>>(a);
   else if (rows == 64) attention_join_kernel<T, WIDTH, 64><<<grid, kBlock, 0, stream>>>(a);

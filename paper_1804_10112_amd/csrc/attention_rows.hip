@@ -44,9 +44,11 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
       missing[stage] = 0;
 #pragma unroll
       for (int x = 0; x < kLoads; ++x) {
-        int64_t place = slot_of(c, entry[x], base + token0 + x * kTokensApart, tokens);
-        if (place < 0) missing[stage] |= 1u << x, place = 0;
-        place += pool + chunk_read * 16;
+        const int t = base + token0 + x * kTokensApart;
+        const bool there = t < tokens && static_cast<unsigned>(entry[x]) < static_cast<unsigned>(c.pages);
+        const uint64_t page = there ? entry[x] : 0, slot = there ? t & ((1 << c.shift) - 1) : 0;
+        const int64_t place = static_cast<int64_t>((page * c.page_vecs + slot * c.slot_vecs + chunk_read) << 4) + pool;
+        missing[stage] |= there ? 0 : 1u << x;
         k[stage][x] = *reinterpret_cast<const i4*>(c.K + place);
         v[stage][x] = *reinterpret_cast<const i4*>(c.V + place);
       }
