@@ -26,6 +26,12 @@ struct Values {
   T v[Vec16<T>::n];
 };
 
+// x / d with 1 / d at hand: the product, corrected once by its remainder. Where that is none (infinities, d = 0), the product.
+__device__ __forceinline__ float quotient(float x, float d, float by_d) {
+  const float q = x * by_d, rest = __builtin_fmaf(-q, d, x);
+  return rest == rest ? __builtin_fmaf(rest, by_d, q) : q;
+}
+
 constexpr int kKept = 8;            // tokens of the sequence that a thread holds in registers; the others are read again for each segment
 constexpr int kNowhere = -(1 << 30);  // below every segment
 
@@ -34,7 +40,7 @@ constexpr int kNowhere = -(1 << 30);  // below every segment
 // order. The sequence's tokens are read at once, into registers, and each segment picks its own; the logits of the next segment are
 // under way while one is counted. A thread clears the counts that it has read, so a segment takes two barriers.
 template <class T, int VECS, bool BIAS>
-__global__ void __launch_bounds__(kThreads) logits_kernel(Logits a) {
+__global__ void __launch_bounds__(kThreads, 8) logits_kernel(Logits a) {
   constexpr int n = Vec16<T>::n, kSegment = kThreads * VECS * n;
   __shared__ __attribute__((aligned(16))) int count[kSegment];
   __shared__ __attribute__((aligned(16))) float bias[BIAS ? kSegment : 4];
@@ -52,7 +58,9 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(Logits a) {
     last = clamped(a.first[s + 1], 0, a.rows);
   }
   const bool aligned = (reinterpret_cast<uintptr_t>(out + ahead) & 15) == 0;
+  const uint32_t* allowed = a.allowed ? a.allowed + r * a.allowed_stride : nullptr;
   Values<T> x[VECS];
+  uint32_t word[VECS][2];  // those with the bits of the first and of the last value
   auto load = [&](int from) {
 #pragma unroll
     for (int k = 0; k < VECS; ++k) {
@@ -63,6 +71,10 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(Logits a) {
 #pragma unroll
         for (int e = 0; e < n; ++e)
           if (v + e >= 0 && v + e < a.cols) x[k].v[e] = in[v + e];
+      }
+      if (allowed && v < a.cols) {
+        word[k][0] = allowed[(v < 0 ? 0 : v) >> 5];
+        word[k][1] = allowed[(v + n - 1 < a.cols ? v + n - 1 : a.cols - 1) >> 5];
       }
     }
   };
@@ -84,7 +96,7 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(Logits a) {
   if (way0 + t < way1) way = way_token(way0 + t);
   if (BIAS && bias0 + t < bias1) at_bias = column(a.bias.crd[bias0 + t]), bias_value = a.bias_vals[bias0 + t];
   const float rep = a.repetition ? a.repetition[s] : 1, pres = a.presence ? a.presence[s] : 0, freq = a.frequency ? a.frequency[s] : 0;
-  const uint32_t* allowed = a.allowed ? a.allowed + r * a.allowed_stride : nullptr;
+  const float by_rep = 1 / rep;
   for (int k = t; k < kSegment / 4; k += kThreads) {
     reinterpret_cast<int4*>(count)[k] = int4{0, 0, 0, 0};
     if (BIAS) reinterpret_cast<float4*>(bias)[k] = float4{0, 0, 0, 0};
@@ -111,8 +123,9 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(Logits a) {
       }
     }
     Values<T> now[VECS];
+    uint32_t now_word[VECS][2];
 #pragma unroll
-    for (int k = 0; k < VECS; ++k) now[k] = x[k];
+    for (int k = 0; k < VECS; ++k) now[k] = x[k], now_word[k][0] = word[k][0], now_word[k][1] = word[k][1];
     const int64_t following = static_cast<int64_t>(lo) + static_cast<int64_t>(gridDim.y) * kSegment;
     const bool more = following < a.cols;
     if (more) load(static_cast<int>(following));
@@ -136,7 +149,7 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(Logits a) {
         for (int e = 0; e < n; e += 4) *reinterpret_cast<int4*>(&count[at + e]) = int4{0, 0, 0, 0};
 #pragma unroll
         for (int e = 0; e < n; ++e)
-          if (c[e]) y[e] = (y[e] > 0 ? y[e] / rep : y[e] * rep) - (pres + freq * static_cast<float>(c[e]));
+          if (c[e]) y[e] = (y[e] > 0 ? quotient(y[e], rep, by_rep) : y[e] * rep) - (pres + freq * static_cast<float>(c[e]));
       }
       if (BIAS)
 #pragma unroll
@@ -146,13 +159,13 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(Logits a) {
           *four = float4{0, 0, 0, 0};
         }
       if (allowed) {
-        const int v0 = v < 0 ? 0 : v, word = v0 >> 5, v1 = v + n - 1 < a.cols ? v + n - 1 : a.cols - 1;
-        const uint64_t bits = (static_cast<uint64_t>(allowed[v1 >> 5]) << ((v1 >> 5) == word ? 0 : 32) | allowed[word]) >> (v0 & 31);
+        // bit e: value e is allowed; values before the row's first have no bits and do not count
+        const int v0 = v < 0 ? 0 : v;
+        const uint64_t both = static_cast<uint64_t>(now_word[k][1]) << 32 | now_word[k][0];
+        const uint32_t bits = static_cast<uint32_t>(both >> (v0 & 31)) << (v0 - v);
 #pragma unroll
-        for (int e = 0; e < n; ++e) {
-          const int b = v + e - v0;
-          if (b >= 0 && !(bits >> b & 1)) y[e] = -INFINITY;
-        }
+        for (int e = 0; e < n; ++e)
+          if (!(bits >> e & 1)) y[e] = -INFINITY;
       }
       Values<T> z;
 #pragma unroll
