@@ -451,8 +451,9 @@ spt_status spt_validate(const spt_tensor* T, int32_t* err_dev, void* stream);
  * negative page number is padding: the tokens of a table entry outside [0, pages) count as absent (never
  * read, written or attended to), and table entries behind the row's last page are not looked at. Numbers in
  * len below 0 count as 0, above page*row_pages as that.
- * refs[p] = number of table rows that list page p; a page with refs 0 is free. Pages are shared by forking; a
- * shared page is read by several rows and, through the entry points here, written by none.
+ * refs[p] = number of table rows that list page p; a page with refs 0 is free. Pages are shared by forking, and
+ * spt_cache_extend gives a row pages of its own for the slots that it makes room in, so what is written to them
+ * (before the next fork) reaches no other row.
  * The V pool has the layout of the K pool: value d of (layer l, page p, slot o, head h) is element
  * l*layer_stride + p*page_stride + o*slot_stride + h*head_stride + d.
  *
@@ -547,7 +548,7 @@ spt_status spt_cache_fork(const spt_cache* c, int64_t n, const int32_t* parents,
  * 32 bits; SPT_F16 and SPT_BF16 multiply in matrix instructions on values of that type, for which exp(z - max)
  * is rounded to it.
  * q, out: T x q_heads x width with the strides given (elements, multiples of 16 bytes; pointers 16-byte aligned),
- * T <= 2^24; q_heads a multiple of heads; lse (may be NULL): float, T x q_heads. The query of the workspace knows no lengths;
+ * T <= 2^24, T * (q_heads/heads) < 2^31 - 256; q_heads a multiple of heads; lse (may be NULL): float, T x q_heads. The query of the workspace knows no lengths;
  * its size does not depend on T. The same call gives the same bits. Workspace: SPT_CACHE_ATTENTION.
  */
 spt_status spt_cache_attention(const spt_cache* c, int32_t layer, const int32_t* first, int64_t T,

@@ -431,6 +431,18 @@ def _use_torch():
     return torch
 
 
+def _on_device(t, device, name):
+    if t.get_device() != device:
+        _invalid(f"{name} is on another device than the rest")
+
+
+def _stream_of(device, stream):
+    """As _stream; a call on torch's current stream is refused where that belongs to another device than the tensors."""
+    if stream is None and device >= 0 and _device is not None and _device() != device:
+        _invalid(f"the tensors are on device {device}, the current device is {_device()}")
+    return _stream(stream)
+
+
 def _i32(t, count, name):
     """Device pointer of a contiguous int32 tensor of at least `count` entries (None -> NULL)."""
     if t is None:
@@ -488,7 +500,9 @@ class DeviceCache:
         c.table, c.len, c.refs = _i32(table, 0, "table"), _i32(length, c.rows, "len"), _i32(refs, c.pages, "refs")
         self.K, self.V, self.table, self.len, self.refs = K, V, table, length, refs
         self.c, self.address = c, C.addressof(c)
-        self.rows, self.heads, self.width, self.dtype = c.rows, c.heads, c.width, K.dtype
+        self.rows, self.heads, self.width, self.dtype, self.device = c.rows, c.heads, c.width, K.dtype, K.get_device()
+        for t, name in ((V, "V"), (table, "table"), (length, "len"), (refs, "refs")):
+            _on_device(t, self.device, name)
 
     def workspace(self, op, q_heads=0):
         import torch
@@ -499,6 +513,7 @@ class DeviceCache:
         shape, stride = t.shape, t.stride()
         if t.dtype is not self.dtype or len(shape) != 3 or shape[2] != self.width or shape[1] != heads or stride[2] != 1:
             _invalid(f"{name} must be (tokens, {heads}, {self.width}), {self.dtype}, values of a head contiguous")
+        _on_device(t, self.device, name)
         return (stride[0] if shape[0] > 1 else 0), (stride[1] if heads > 1 else 0)
 
 
@@ -512,7 +527,7 @@ def spt_cache_workspace_bytes(op, cache, q_heads=0) -> int:
 def spt_cache_extend(cache, add, refused_dev, ws=None, stream=None):
     p, n = _ws(ws)
     _check(lib().spt_cache_extend(cache.address, _i32(add, cache.rows, "add"), _i32(refused_dev, 1, "refused_dev"), p, n,
-                                  _stream(stream)))
+                                  _stream_of(cache.device, stream)))
 
 
 def spt_cache_write(cache, layer, first, k, v, stream=None):
@@ -521,20 +536,20 @@ def spt_cache_write(cache, layer, first, k, v, stream=None):
     if cache._tokens(v, "v", cache.heads) != (token, head) or v.shape[0] != tokens:
         _invalid("k and v must be alike")
     _check(lib().spt_cache_write(cache.address, layer, _i32(first, cache.rows + 1, "first"), tokens, k.data_ptr(), v.data_ptr(), token,
-                                 head, _stream(stream)))
+                                 head, _stream_of(cache.device, stream)))
 
 
 def spt_cache_compact(cache, first, keep, stream=None):
-    _check(lib().spt_cache_compact(cache.address, _i32(first, cache.rows + 1, "first"), keep and _desc(keep), _stream(stream)))
+    _check(lib().spt_cache_compact(cache.address, _i32(first, cache.rows + 1, "first"), keep and _desc(keep), _stream_of(cache.device, stream)))
 
 
 def spt_cache_free(cache, new_len, stream=None):
-    _check(lib().spt_cache_free(cache.address, _i32(new_len, cache.rows, "new_len"), _stream(stream)))
+    _check(lib().spt_cache_free(cache.address, _i32(new_len, cache.rows, "new_len"), _stream_of(cache.device, stream)))
 
 
 def spt_cache_fork(cache, parents, children, stream=None):
     n = children.numel()
-    _check(lib().spt_cache_fork(cache.address, n, _i32(parents, n, "parents"), _i32(children, n, "children"), _stream(stream)))
+    _check(lib().spt_cache_fork(cache.address, n, _i32(parents, n, "parents"), _i32(children, n, "children"), _stream_of(cache.device, stream)))
 
 
 def spt_cache_attention(cache, layer, first, tree, q, scale, out, lse=None, ws=None, stream=None):
@@ -551,7 +566,7 @@ def spt_cache_attention(cache, layer, first, tree, q, scale, out, lse=None, ws=N
     p, n = _ws(ws)
     _check(lib().spt_cache_attention(cache.address, layer, _i32(first, cache.rows + 1, "first"), shape[0], tree and _desc(tree),
                                      q.data_ptr(), heads, q_token, q_head, scale, out.data_ptr(), out_token, out_head, _p(lse), p, n,
-                                     _stream(stream)))
+                                     _stream_of(cache.device, stream)))
 
 
 class LogitRules:
@@ -597,7 +612,8 @@ def spt_adjust_logits(logits, rules, out, stream=None):
         _invalid("the values of a row of logits and out must be contiguous")
     if R <= 1:
         stride = out_stride = V
+    _on_device(out, logits.get_device(), "out")
     if rules.rows is not None and rules.rows < R:
         _invalid("drafts or allowed have fewer rows than logits")
     _check(lib().spt_adjust_logits(_dtype_code(dtype), R, V, logits.data_ptr(), stride, rules.address, out.data_ptr(), out_stride,
-                                   _stream(stream)))
+                                   _stream_of(logits.get_device(), stream)))

@@ -191,6 +191,9 @@ spt_status spt_cache_attention(const spt_cache* c, int32_t layer, const int32_t*
   if (q_heads < 1 || q_heads > 65535 || q_heads % c->heads != 0)
     return fail(SPT_ERR_INVALID_ARG, "cache_attention: q_heads %d is not a multiple of the cache's %d heads, up to 65535", q_heads,
                 c->heads);
+  if (T * (q_heads / c->heads) >= INT32_MAX - 256)
+    return fail(SPT_ERR_UNSUPPORTED, "cache_attention: %lld tokens of %d query heads for each head of K", (long long)T,
+                q_heads / c->heads);
   if (tree) {
     st = pattern_ok(tree, T, "cache_attention", "tree");
     if (st != SPT_OK) return st;

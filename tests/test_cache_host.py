@@ -54,7 +54,7 @@ BAD_CACHES = [
     (dict(page=24), 2), (dict(page=1 << 17), 2), (dict(rows=-1), 1), (dict(row_pages=-1), 1), (dict(pages=-1), 1),
     (dict(pages=2 ** 31 - 1), 1), (dict(rows=(1 << 20) + 1, row_pages=1), 2), (dict(rows=1 << 20, row_pages=1 << 11), 2),
     (dict(row_pages=1 << 27), 2), (dict(slot_stride=-256), 1), (dict(head_stride=60), 1), (dict(page_stride=4), 1),
-    (dict(layer_stride=1 << 41), 1), (dict(K=None), 1), (dict(V=None), 1), (dict(refs=None), 1), (dict(table=None), 1),
+    (dict(layer_stride=1 << 41), 1), (dict(page_stride=1 << 33), 2), (dict(layers=65536, heads=2), 2), (dict(K=None), 1), (dict(V=None), 1), (dict(refs=None), 1), (dict(table=None), 1),
     (dict(len=None), 1), (dict(K=FAKE + 8), 1), (dict(V=FAKE + 2), 1), (dict(dtype=B.SPT_F32, head_stride=62), 1),
 ]
 
@@ -137,11 +137,12 @@ def test_refusals_of_attention():
     need = lib.spt_cache_workspace_bytes(B.SPT_CACHE_ATTENTION, C.addressof(c), 8)
 
     def call(layer=0, first=FAKE, T=5, tree=None, q=FAKE, heads=8, qt=512, qh=64, out=FAKE, ot=512, oh=64):
-        return lib.spt_cache_attention(C.addressof(c), layer, first, T, _addr(tree), q, heads, qt, qh, 1.0, out, ot, oh, None, FAKE, need, None)
+        return lib.spt_cache_attention(C.addressof(c), layer, first, T, _addr(tree), q, heads, qt, qh, 1.0, out, ot, oh, None, FAKE,
+                                       need, None)
 
     assert [call(layer=2), call(T=-1), call(first=None), call(q=None), call(out=None), call(heads=6), call(heads=0), call(q=FAKE + 2),
             call(out=FAKE + 8), call(qt=-8), call(qh=3), call(ot=7), call(oh=-64), call(tree=_csr(4)), call(tree=_csr(6))] == [1] * 15
-    assert call(T=(1 << 24) + 1) == 2
+    assert call(T=(1 << 24) + 1) == 2 and call(T=1 << 24, heads=4 * 1024) == 2
     csc = _csr(5)
     csc.level[0].mode, csc.level[1].mode = 1, 0
     assert call(tree=csc) == 2
@@ -161,7 +162,7 @@ def test_refusals_of_logits():
     assert call(dtype=B.SPT_F64) == 2 and call(dtype=5) == 1 and call(rules=False) == 1
     assert [call(R=-1), call(V=-1), call(V=2 ** 31 - 1), call(sequences=-1), call(first=None), call(stride=99), call(out_stride=99),
             call(logits=None), call(out=None), call(logits=FAKE + 1), call(dtype=B.SPT_F32, out=FAKE + 2), call(out_stride=108)] == [1] * 12
-    assert call(R=(1 << 24) + 1) == 2
+    assert call(R=(1 << 24) + 1) == 2 and call(V=(1 << 27) + 1, stride=1 << 28, out_stride=1 << 28) == 2
     assert call(seen=_csr(3)) == 1 and call(tree=_csr(3)) == 1 and call(tree=_csr(2), drafts=FAKE) == 1
     assert call(bias=_csr(3)) == 1 and call(bias=_csr(2, dtype=1)) == 2 and call(bias=_csr(2, flags=1)) == 2
     assert call(bias=_csr(2, vals=None)) == 1

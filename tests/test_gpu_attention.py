@@ -67,7 +67,7 @@ def test_rows_that_see_nothing(dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-@pytest.mark.parametrize("context,drafts", [(0, 6), (45, 6), (100, 70)])
+@pytest.mark.parametrize("context,drafts", [(0, 6), (45, 6), (45, 20), (0, 40), (77, 40), (100, 70)])
 def test_what_a_token_does_not_see_does_not_reach_it(dtype, bad, context, drafts):
     """Infinities and NaNs in keys and values of drafted tokens that some see and others do not; every draft sees itself, so the
     bad one's own row is bad, and those below it."""
@@ -185,8 +185,8 @@ def test_offsets_beyond_32_bits():
     for view, data in zip(views, (small.K, small.V)):
         view.copy_(data.cuda())
     far = spt.DeviceCache(views[0], views[1], cache.table, cache.len, cache.refs)
-    q = random_q(5, 2, 64, "bf16", 3)
-    for layer in range(2):
+    for layer, q_heads in ((0, 2), (1, 2), (1, 16), (0, 40)):       # one kernel for few rows, one for many
+        q = random_q(5, q_heads, 64, "bf16", 3)
         near = gpu_attention(cache, layer, [3, 2], None, q, 0.1)
         got = gpu_attention(far, layer, [3, 2], None, q, 0.1)
         assert torch.equal(near[0], got[0]) and torch.equal(near[1], got[1])
@@ -261,3 +261,57 @@ def test_two_streams_with_a_workspace_each():
     torch.cuda.synchronize()
     for o in outs:
         assert torch.equal(o.cpu(), want[0])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 1.0, 1e-30])
+def test_scales(dtype, scale):
+    """Negative ones turn the order round, 0 weighs everything seen alike."""
+    for drafts in (2, 20, 60):
+        counts = [drafts, 3]
+        host = HostCache([drafts + 70, 9], 16, 2, 64, dtype, seed=drafts)
+        check_attention(host, counts, random_tree(counts, 4), 4, scale=scale, what=f"scale {scale}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("drafts", [1, 17, 30, 70])
+@pytest.mark.parametrize("width", [72, 128, 200])
+def test_pages_that_are_missing_and_ends_of_steps(dtype, drafts, width):
+    """Pages outside the pool at the beginning, within and at the end of a row, lengths around a step of 64 and 128 tokens."""
+    for length in (drafts + 63, drafts + 64, drafts + 129):
+        host = HostCache([length, length + 1], 8, 1, width, dtype, seed=length)
+        host.table[0][0], host.table[0][5], host.table[1][(length + 1 - 1) // 8] = -1, 1 << 20, -5
+        check_attention(host, [drafts, drafts], None, 2, what=f"{length} {drafts}")
+
+
+def test_rows_of_very_different_sizes_in_one_call():
+    """A chunk of a prompt beside rows that decode: one kernel serves both, whichever the mean chooses."""
+    counts = [200] + [1] * 12 + [0] * 60 + [31]
+    lens = [260] + [int(x) for x in np.random.default_rng(1).integers(1, 400, 12)] + [5] * 60 + [400]
+    host = HostCache(lens, 16, 2, 64, "bf16", seed=1)
+    check_attention(host, counts, None, 8, what="mixed, few")
+    host = HostCache(lens[:3], 16, 2, 64, "bf16", seed=2)
+    check_attention(host, counts[:3], None, 8, what="mixed, many")
+
+
+def test_one_workspace_for_calls_of_several_shapes():
+    """A workspace is scratch: calls of other sizes, with the same one, in turn give what each gives alone."""
+    import paper_1804_10112_amd as spt
+    host = HostCache([900, 40, 333], 16, 2, 128, "bf16", seed=5)
+    cache = host.device()
+    ws = cache.workspace(spt.SPT_CACHE_ATTENTION, 8)
+    cases = []
+    for counts in ([1, 1, 1], [40, 3, 9], [130, 40, 2], [5, 0, 0]):
+        q = random_q(sum(counts), 8, 128, "bf16", sum(counts)).cuda()
+        first = torch.tensor(offsets(counts), dtype=torch.int32, device="cuda")
+        alone = torch.empty_like(q)
+        spt.spt_cache_attention(cache, 0, first, None, q, 0.1, alone, None, cache.workspace(spt.SPT_CACHE_ATTENTION, 8))
+        cases.append((q, first, alone))
+    torch.cuda.synchronize()
+    outs = [torch.empty_like(q) for q, _, _ in cases]
+    for _ in range(3):
+        for (q, first, _), out in zip(cases, outs):
+            spt.spt_cache_attention(cache, 0, first, None, q, 0.1, out, None, ws)
+    torch.cuda.synchronize()
+    for (_, _, alone), out in zip(cases, outs):
+        assert torch.equal(alone, out)
