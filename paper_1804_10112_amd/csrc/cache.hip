@@ -136,7 +136,9 @@ __device__ __forceinline__ void assign(const Cache& c, const int32_t* __restrict
   if (place == 0) plan.target[s] = p;
 }
 
-constexpr int kHeld = 16;  // refs that a thread holds of a small pool
+// Refs that a thread holds of a small pool. Pools of 1000 to 4000 pages take 11.2 us either way, with the freeing after it (replayed); one
+// launch less to make is what counts. At 16 000 pages one workgroup takes 12.9 us, two launches 11.3.
+constexpr int kHeld = 4;
 
 __global__ void __launch_bounds__(kScanBlock) extend_small_kernel(Cache c, const int32_t* __restrict__ add, Plan plan,
                                                                   int32_t* refused) {
