@@ -10,7 +10,12 @@
 // The work of a call is all steps of all tiles, a number that only the device knows (lengths change between calls of one captured
 // graph). Each workgroup of a fixed grid finds its equal share of it from len and first: a range of steps that may begin and end
 // within a tile. A tile that lies in one workgroup goes to `out` at once; one that does not leaves m, l and O of each part in the
-// workspace, at most two parts a workgroup, and a second kernel joins them.
+// workspace, at most two parts a workgroup, and a second kernel joins them. 512 workgroups, all that run at once: 1024, to even out
+// which of them end first, took 4 % longer on a decoding batch and 30 % longer on trees, each having its own start and parts.
+//
+// What bounds it: the reading of K and V, up to some 250 rows a sequence (1.33 GB of a decoding batch of 64 rows: 265 us and 5 for the
+// joining, 4.9 TB/s, what a large copy reaches), the matrix products and the softmax beyond (chunks of 1024 tokens: 584 TFLOP/s, half of a
+// large matrix product's), and in small calls the way to the first load: some 8 us in a workgroup, 4 for the joining.
 #pragma once
 #include "cache.hpp"
 #include "values.hpp"

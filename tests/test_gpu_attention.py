@@ -315,3 +315,15 @@ def test_one_workspace_for_calls_of_several_shapes():
     torch.cuda.synchronize()
     for (_, _, alone), out in zip(cases, outs):
         assert torch.equal(alone, out)
+
+
+@pytest.mark.parametrize("counts", [[1, 1, 1], [40, 3, 9], [90, 40, 2]])
+def test_results_in_place_of_the_queries(counts):
+    import paper_1804_10112_amd as spt
+    host = HostCache([700, 40, 333], 16, 2, 64, "bf16", seed=5)
+    cache, q = host.device(), random_q(sum(counts), 8, 64, "bf16", 2)
+    want = gpu_attention(cache, 0, counts, None, q, 0.1, extra=0)[0]
+    first, qd = torch.tensor(offsets(counts), dtype=torch.int32, device="cuda"), q.cuda()
+    spt.spt_cache_attention(cache, 0, first, None, qd, 0.1, qd, None, cache.workspace(spt.SPT_CACHE_ATTENTION, 8))
+    torch.cuda.synchronize()
+    assert torch.equal(qd.cpu(), want)
