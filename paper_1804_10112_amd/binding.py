@@ -586,18 +586,23 @@ class LogitRules:
         for t in per_sequence:
             if t.dtype != torch.float32 or not t.is_contiguous() or t.numel() < sequences:
                 _invalid(f"repetition, presence and frequency must be contiguous float32 tensors of {sequences} entries")
-        if allowed is not None and (allowed.dtype not in (torch.int32, torch.uint32) or allowed.dim() != 2 or
-                                    _stride(allowed, 1) not in (0, 1)):
-            _invalid("allowed must be (rows, words) of 32 bits")
+        if allowed is not None:
+            if allowed.dtype not in (torch.int32, torch.uint32) or allowed.dim() != 2:
+                _invalid("allowed must be (rows, words) of 32 bits")
+            rows, words = allowed.shape
+            # one mask for all rows (expand) has stride 0, which no rule has: it would be read as rows side by side
+            if (words > 1 and allowed.stride(1) != 1) or (rows > 1 and allowed.stride(0) < words):
+                _invalid("the words of a row of allowed must be contiguous, its rows apart")
         r = SptLogitRules()
         r.first, r.sequences = _i32(first, sequences + 1, "first"), sequences
         r.seen, r.tree, r.bias = (m and _desc(m) for m in (seen, tree, bias))
         r.drafts = _i32(drafts, 0, "drafts")
         r.repetition, r.presence, r.frequency = _p(repetition), _p(presence), _p(frequency)
         if allowed is not None:
-            r.allowed, r.allowed_stride = allowed.data_ptr(), max(_stride(allowed, 0), allowed.shape[1])
+            r.allowed, r.allowed_stride = allowed.data_ptr(), allowed.stride(0) if rows > 1 else words
         self.keep = (first, seen, tree, drafts, repetition, presence, frequency, bias, allowed)
         self.rows = min([t.shape[0] for t in (drafts, allowed) if t is not None], default=None)
+        self.columns = None if allowed is None else 32 * words
         self.c, self.address = r, C.addressof(r)
 
 
@@ -615,5 +620,7 @@ def spt_adjust_logits(logits, rules, out, stream=None):
     _on_device(out, logits.get_device(), "out")
     if rules.rows is not None and rules.rows < R:
         _invalid("drafts or allowed have fewer rows than logits")
+    if rules.columns is not None and rules.columns < V:
+        _invalid(f"allowed has {rules.columns // 32} words a row, {V} logits need {(V + 31) // 32}")
     _check(lib().spt_adjust_logits(_dtype_code(dtype), R, V, logits.data_ptr(), stride, rules.address, out.data_ptr(), out_stride,
                                    _stream_of(logits.get_device(), stream)))
