@@ -437,19 +437,49 @@ def _on_device(t, device, name):
 
 
 def _stream_of(device, stream):
-    """As _stream; a call on torch's current stream is refused where that belongs to another device than the tensors."""
-    if stream is None and device >= 0 and _device is not None and _device() != device:
+    """As _stream, for tensors that all lie on `device`: refused are tensors on the host, torch's current stream where another device
+    is the current one, and a stream of torch's that belongs to another device (a plain handle does not say to which it belongs)."""
+    if device < 0:
+        _invalid("the tensors are not on a GPU")
+    if stream is not None:
+        if getattr(stream, "device_index", device) != device:
+            _invalid(f"the tensors are on device {device}, the stream is of device {stream.device_index}")
+        return _stream(stream)
+    handle = _current_stream()  # finds out how to ask for the current device, in a process's first call
+    if _device is not None and _device() != device:
         _invalid(f"the tensors are on device {device}, the current device is {_device()}")
-    return _stream(stream)
+    return handle
 
 
-def _i32(t, count, name):
-    """Device pointer of a contiguous int32 tensor of at least `count` entries (None -> NULL)."""
+def _i32(t, count, name, device=None):
+    """Pointer of a contiguous int32 tensor of at least `count` entries, on `device` if that is given (None -> NULL)."""
     if t is None:
         return None
     if t.dtype is not _int32 or t.numel() < count or not t.is_contiguous():
         _invalid(f"{name} must be a contiguous int32 tensor of at least {count} entries")
+    if device is not None:
+        _on_device(t, device, name)
     return t.data_ptr()
+
+
+def _matrix_device(m):
+    """The device of a sparse matrix, None of a plain descriptor, which does not say it."""
+    return m.device if isinstance(m, DeviceCSR) else m.vals.get_device() if isinstance(m, DeviceTensor) else None
+
+
+def _matrix(m, device, name):
+    """Descriptor of a sparse matrix that lies on `device` (None -> NULL)."""
+    if m is None:
+        return None
+    if _matrix_device(m) not in (device, None):
+        _invalid(f"{name} is on another device than the rest")
+    return _desc(m)
+
+
+def _ws_on(ws, device):
+    if ws is not None and not isinstance(ws, int):
+        _on_device(ws, device, "the workspace")
+    return _ws(ws)
 
 
 def _stride(t, d):
@@ -471,9 +501,12 @@ class DeviceCSR:
         o = t.level[1]
         o.kind, o.mode, o.N, o.M = 1, 1, int(cols), rows
         o.flags = (SPT_ORDERED if ordered else 0) | (SPT_UNIQUE if unique else 0)
-        o.pos, o.crd = _i32(pos, 1, "pos"), _i32(crd, 0, "crd")
-        if vals is not None and (vals.numel() != crd.numel() or not vals.is_contiguous()):
-            _invalid("vals must be contiguous, one value for each entry of crd")
+        self.device = pos.get_device()
+        o.pos, o.crd = _i32(pos, 1, "pos"), _i32(crd, 0, "crd", self.device)
+        if vals is not None:
+            if vals.numel() != crd.numel() or not vals.is_contiguous():
+                _invalid("vals must be contiguous, one value for each entry of crd")
+            _on_device(vals, self.device, "vals")
         t.vals, t.nvals = _p(vals), crd.numel()
         self.keep = (pos, crd, vals)
         self.c = t
@@ -525,9 +558,10 @@ def spt_cache_workspace_bytes(op, cache, q_heads=0) -> int:
 
 
 def spt_cache_extend(cache, add, refused_dev, ws=None, stream=None):
-    p, n = _ws(ws)
-    _check(lib().spt_cache_extend(cache.address, _i32(add, cache.rows, "add"), _i32(refused_dev, 1, "refused_dev"), p, n,
-                                  _stream_of(cache.device, stream)))
+    device = cache.device
+    p, n = _ws_on(ws, device)
+    _check(lib().spt_cache_extend(cache.address, _i32(add, cache.rows, "add", device), _i32(refused_dev, 1, "refused_dev", device), p, n,
+                                  _stream_of(device, stream)))
 
 
 def spt_cache_write(cache, layer, first, k, v, stream=None):
@@ -535,21 +569,26 @@ def spt_cache_write(cache, layer, first, k, v, stream=None):
     tokens = k.shape[0]
     if cache._tokens(v, "v", cache.heads) != (token, head) or v.shape[0] != tokens:
         _invalid("k and v must be alike")
-    _check(lib().spt_cache_write(cache.address, layer, _i32(first, cache.rows + 1, "first"), tokens, k.data_ptr(), v.data_ptr(), token,
-                                 head, _stream_of(cache.device, stream)))
+    device = cache.device
+    _check(lib().spt_cache_write(cache.address, layer, _i32(first, cache.rows + 1, "first", device), tokens, k.data_ptr(), v.data_ptr(),
+                                 token, head, _stream_of(device, stream)))
 
 
 def spt_cache_compact(cache, first, keep, stream=None):
-    _check(lib().spt_cache_compact(cache.address, _i32(first, cache.rows + 1, "first"), keep and _desc(keep), _stream_of(cache.device, stream)))
+    device = cache.device
+    _check(lib().spt_cache_compact(cache.address, _i32(first, cache.rows + 1, "first", device), _matrix(keep, device, "keep"),
+                                   _stream_of(device, stream)))
 
 
 def spt_cache_free(cache, new_len, stream=None):
-    _check(lib().spt_cache_free(cache.address, _i32(new_len, cache.rows, "new_len"), _stream_of(cache.device, stream)))
+    device = cache.device
+    _check(lib().spt_cache_free(cache.address, _i32(new_len, cache.rows, "new_len", device), _stream_of(device, stream)))
 
 
 def spt_cache_fork(cache, parents, children, stream=None):
-    n = children.numel()
-    _check(lib().spt_cache_fork(cache.address, n, _i32(parents, n, "parents"), _i32(children, n, "children"), _stream_of(cache.device, stream)))
+    n, device = children.numel(), cache.device
+    _check(lib().spt_cache_fork(cache.address, n, _i32(parents, n, "parents", device), _i32(children, n, "children", device),
+                                _stream_of(device, stream)))
 
 
 def spt_cache_attention(cache, layer, first, tree, q, scale, out, lse=None, ws=None, stream=None):
@@ -560,13 +599,15 @@ def spt_cache_attention(cache, layer, first, tree, q, scale, out, lse=None, ws=N
     out_token, out_head = cache._tokens(out, "out", heads)
     if out.shape != shape:
         _invalid("q and out have different numbers of tokens")
-    if lse is not None and (lse.shape != shape[:2] or lse.element_size() != 4 or not lse.is_floating_point()
-                            or not lse.is_contiguous()):
-        _invalid("lse must be float32, (tokens, q_heads), contiguous")
-    p, n = _ws(ws)
-    _check(lib().spt_cache_attention(cache.address, layer, _i32(first, cache.rows + 1, "first"), shape[0], tree and _desc(tree),
-                                     q.data_ptr(), heads, q_token, q_head, scale, out.data_ptr(), out_token, out_head, _p(lse), p, n,
-                                     _stream_of(cache.device, stream)))
+    device = cache.device
+    if lse is not None:
+        if lse.shape != shape[:2] or lse.element_size() != 4 or not lse.is_floating_point() or not lse.is_contiguous():
+            _invalid("lse must be float32, (tokens, q_heads), contiguous")
+        _on_device(lse, device, "lse")
+    p, n = _ws_on(ws, device)
+    _check(lib().spt_cache_attention(cache.address, layer, _i32(first, cache.rows + 1, "first", device), shape[0],
+                                     _matrix(tree, device, "tree"), q.data_ptr(), heads, q_token, q_head, scale, out.data_ptr(), out_token,
+                                     out_head, _p(lse), p, n, _stream_of(device, stream)))
 
 
 class LogitRules:
@@ -593,6 +634,11 @@ class LogitRules:
             # one mask for all rows (expand) has stride 0, which no rule has: it would be read as rows side by side
             if (words > 1 and allowed.stride(1) != 1) or (rows > 1 and allowed.stride(0) < words):
                 _invalid("the words of a row of allowed must be contiguous, its rows apart")
+        devices = {t.get_device() for t in (first, drafts, *per_sequence, allowed) if t is not None}
+        devices |= {_matrix_device(m) for m in (seen, tree, bias) if m is not None} - {None}
+        if len(devices) > 1:
+            _invalid("the rules are on several devices")
+        self.device = devices.pop() if devices else None
         r = SptLogitRules()
         r.first, r.sequences = _i32(first, sequences + 1, "first"), sequences
         r.seen, r.tree, r.bias = (m and _desc(m) for m in (seen, tree, bias))
@@ -617,10 +663,13 @@ def spt_adjust_logits(logits, rules, out, stream=None):
         _invalid("the values of a row of logits and out must be contiguous")
     if R <= 1:
         stride = out_stride = V
-    _on_device(out, logits.get_device(), "out")
+    device = logits.get_device()
+    _on_device(out, device, "out")
+    if rules.device is not None and rules.device != device:
+        _invalid("the rules are on another device than the logits")
     if rules.rows is not None and rules.rows < R:
         _invalid("drafts or allowed have fewer rows than logits")
     if rules.columns is not None and rules.columns < V:
         _invalid(f"allowed has {rules.columns // 32} words a row, {V} logits need {(V + 31) // 32}")
     _check(lib().spt_adjust_logits(_dtype_code(dtype), R, V, logits.data_ptr(), stride, rules.address, out.data_ptr(), out_stride,
-                                   _stream_of(logits.get_device(), stream)))
+                                   _stream_of(device, stream)))
