@@ -287,14 +287,14 @@ __device__ __forceinline__ uint32_t row_sight(const Attention& a, const Q& q, in
   } else if (!a.tree.pos) {
     bits = low_bits(q.context + token + 1 - base);
   } else if (base + 32 > q.context) {
-    const int r = q.d.begin + token, end = pattern_end(a.tree, r);
-    for (int e = pattern_begin(a.tree, r) + quad; e < end; e += 4) {
+    const int r = q.d.begin + token;
+    strided(pattern_begin(a.tree, r), pattern_end(a.tree, r), quad, 4, [&](int e) {
       const int j = a.tree.crd[e];
       if (j >= 0 && j < q.d.count) {
         const int b = q.context + j - base;
         if (b >= 0 && b < 32) bits |= 1u << b;
       }
-    }
+    });
   }
   bits |= __shfl_xor(bits, 16);
   bits |= __shfl_xor(bits, 32);

@@ -94,9 +94,9 @@ __global__ void __launch_bounds__(kThreads, 8) logits_kernel(Logits a) {
   int token[kKept], way = kNowhere, at_bias = kNowhere;
   float bias_value = 0;
 #pragma unroll
-  for (int k = 0; k < kKept; ++k) token[k] = seen0 + k * kThreads + t < seen1 ? a.seen.crd[seen0 + k * kThreads + t] : kNowhere;
-  if (way0 + t < way1) way = way_token(way0 + t);
-  if (BIAS && bias0 + t < bias1) at_bias = column(a.bias.crd[bias0 + t]), bias_value = a.bias_vals[bias0 + t];
+  for (int k = 0; k < kKept; ++k) token[k] = k * kThreads + t < seen1 - seen0 ? a.seen.crd[seen0 + k * kThreads + t] : kNowhere;
+  if (t < way1 - way0) way = way_token(way0 + t);
+  if (BIAS && t < bias1 - bias0) at_bias = column(a.bias.crd[bias0 + t]), bias_value = a.bias_vals[bias0 + t];
   const float rep = a.repetition ? a.repetition[s] : 1, pres = a.presence ? a.presence[s] : 0, freq = a.frequency ? a.frequency[s] : 0;
   const float by_rep = 1 / rep;
   for (int k = t; k < kSegment / 4; k += kThreads) {
@@ -114,15 +114,15 @@ __global__ void __launch_bounds__(kThreads, 8) logits_kernel(Logits a) {
     };
 #pragma unroll
     for (int k = 0; k < kKept; ++k) add(token[k]);
-    for (int e = seen0 + kKept * kThreads + t; e < seen1; e += kThreads) add(column(a.seen.crd[e]));
+    strided(seen0, seen1, kKept * kThreads + t, kThreads, [&](int e) { add(column(a.seen.crd[e])); });
     add(way);
-    for (int e = way0 + kThreads + t; e < way1; e += kThreads) add(way_token(e));
+    strided(way0, way1, kThreads + t, kThreads, [&](int e) { add(way_token(e)); });
     if (BIAS) {
       if (static_cast<unsigned>(at_bias - lo) < width) bias[at_bias - lo] = bias_value;
-      for (int e = bias0 + kThreads + t; e < bias1; e += kThreads) {
+      strided(bias0, bias1, kThreads + t, kThreads, [&](int e) {
         const int v = column(a.bias.crd[e]);
         if (static_cast<unsigned>(v - lo) < width) bias[v - lo] = a.bias_vals[e];
-      }
+      });
     }
     Values<T> now[VECS];
     uint32_t now_word[VECS][2];
