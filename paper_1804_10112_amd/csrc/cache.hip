@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(kScanBlock) extend_count_kernel(Cache c, const
   }
   const int lo = blockIdx.x * stretch, hi = c.pages - lo < stretch ? c.pages : lo + stretch;
   int n = 0;
-  for (int p = lo + threadIdx.x; p < hi; p += kScanBlock) n += c.refs[p] == 0;
+  strided(lo, hi, threadIdx.x, kScanBlock, [&](int p) { n += c.refs[p] == 0; });
   n = block_inclusive_scan(n, lds);
   if (threadIdx.x == kScanBlock - 1) plan.free_pages[blockIdx.x] = n;
 }
@@ -213,9 +213,10 @@ __global__ void __launch_bounds__(kScanBlock) extend_assign_kernel(Cache c, cons
   const int total = sums[1];
   if (blockIdx.x == 0 && threadIdx.x == 0) *plan.total = total;
   const int needed = plan.end[c.rows - 1];
-  const int lo = blockIdx.x * stretch, hi = c.pages - lo < stretch ? c.pages : lo + stretch;
-  for (int base = lo; base < hi && rank < needed; base += kScanBlock) {
-    const int p = base + threadIdx.x;
+  const int lo = blockIdx.x * stretch;
+  const uint32_t hi = c.pages - lo < stretch ? c.pages : lo + stretch;
+  for (uint32_t base = lo; base < hi && rank < needed; base += kScanBlock) {  // a step past the last page may pass 2^31
+    const uint32_t p = base + threadIdx.x;
     const int is_free = p < hi && c.refs[p] == 0;
     const int upto = rank + block_inclusive_scan(is_free, lds);
     if (is_free && upto <= needed) assign(c, add, plan, p, upto - 1, total);
@@ -375,7 +376,7 @@ spt_status cache_extend_dispatch(const spt_cache* cache, const int32_t* add, int
   if (c.pages <= kHeld * kScanBlock) {
     extend_small_kernel<<<1, kScanBlock, 0, stream>>>(c, add, plan, refused);
   } else {
-    const int stretch = stretch_of(c.pages), blocks = (c.pages + stretch - 1) / stretch;
+    const int stretch = stretch_of(c.pages), blocks = (c.pages - 1) / stretch + 1;
     extend_count_kernel<<<blocks + 1, kScanBlock, 0, stream>>>(c, add, stretch, plan, refused);
     if (c.rows > 0) extend_assign_kernel<<<blocks, kScanBlock, 0, stream>>>(c, add, stretch, plan);
   }

@@ -60,3 +60,22 @@ def test_trees_whose_entries_end_where_int32_does(entries, dtype, q_heads):
     ref, ref_lse, bound, lse_bound = attention_reference(host, 0, [3], rows, q, 0.125)
     assert_within(out, ref, bound, "out")
     assert_within(lse, ref_lse, lse_bound, "lse")
+
+
+@pytest.mark.parametrize("pages", [MOST, MOST - 1023, MOST - 2 ** 21])
+def test_pools_of_as_many_pages_as_one_may_have(pages):
+    """The free pages are the last ones; the pages' slots overlap (a stride of 0), of which extending without sharing moves none."""
+    import paper_1804_10112_amd as spt
+    refs = torch.ones(pages, dtype=torch.int32, device="cuda")
+    refs[-3:], refs[5] = 0, 0
+    pool = torch.zeros(8, device="cuda").as_strided((1, pages, 1, 1, 8), (8, 0, 8, 8, 1))
+    cache = spt.DeviceCache(pool, pool, torch.full((3, 3), -1, dtype=torch.int32, device="cuda"), i32([0, 0, 0]), refs)
+    refused = i32([-1])
+    spt.spt_cache_extend(cache, i32([3, 2, 1]), refused, cache.workspace(spt.SPT_CACHE_EXTEND))
+    assert cache.table.tolist() == [[5, pages - 3, pages - 2], [-1, -1, -1], [-1, -1, -1]]
+    assert cache.len.tolist() == [3, 0, 0] and int(refused.item()) == 2
+    spt.spt_cache_extend(cache, i32([0, 1, 1]), refused, cache.workspace(spt.SPT_CACHE_EXTEND))
+    assert cache.table.tolist() == [[5, pages - 3, pages - 2], [pages - 1, -1, -1], [-1, -1, -1]] and int(refused.item()) == 1
+    assert refs[-3:].tolist() == [1, 1, 1] and int(refs[5]) == 1
+    del refs, cache
+    torch.cuda.empty_cache()
