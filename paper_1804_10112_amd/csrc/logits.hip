@@ -11,6 +11,7 @@ struct Logits {
   void* out;
   int64_t in_stride, out_stride, allowed_stride;
   int rows, cols, sequences;
+  int row0;  // of the launch
   const int32_t* first;
   Pattern seen, tree, bias;
   const float* bias_vals;
@@ -46,7 +47,7 @@ __global__ void __launch_bounds__(kThreads, 8) logits_kernel(Logits a) {
   constexpr int n = Vec16<T>::n, kSegment = kThreads * VECS * n;
   __shared__ __attribute__((aligned(16))) int count[kSegment];
   __shared__ __attribute__((aligned(16))) float bias[BIAS ? kSegment : 4];
-  const int r = blockIdx.x;
+  const int r = a.row0 + static_cast<int>(blockIdx.x);
   const T* in = static_cast<const T*>(a.in) + r * a.in_stride;
   T* out = static_cast<T*>(a.out) + r * a.out_stride;
   const int ahead = static_cast<int>(-reinterpret_cast<intptr_t>(in) / static_cast<int>(sizeof(T))) & (n - 1);
@@ -186,15 +187,21 @@ __global__ void __launch_bounds__(kThreads, 8) logits_kernel(Logits a) {
   }
 }
 
+// A launch holds fewer than 2^32 threads in a direction: less than 2^23 rows of 512.
+constexpr int kRowsAtOnce = 1 << 22;
+
 template <class T, int VECS>
-void launch(const Logits& a, int most, hipStream_t stream) {
+void launch(Logits a, int most, hipStream_t stream) {
   constexpr int segment = kThreads * VECS * Vec16<T>::n;
   // a row that begins in the middle of 16 bytes has up to 15 bytes more
   const int64_t segments = (static_cast<int64_t>(a.cols) + Vec16<T>::n - 1 + segment - 1) / segment;
   const int64_t parts = a.rows < most ? most / a.rows : 1;
-  const dim3 grid(a.rows, static_cast<unsigned>(parts < segments ? parts : segments));
-  if (a.bias.pos) logits_kernel<T, VECS, true><<<grid, kThreads, 0, stream>>>(a);
-  else logits_kernel<T, VECS, false><<<grid, kThreads, 0, stream>>>(a);
+  for (; a.row0 < a.rows; a.row0 += kRowsAtOnce) {
+    const int rows = a.rows - a.row0 < kRowsAtOnce ? a.rows - a.row0 : kRowsAtOnce;
+    const dim3 grid(rows, static_cast<unsigned>(parts < segments ? parts : segments));
+    if (a.bias.pos) logits_kernel<T, VECS, true><<<grid, kThreads, 0, stream>>>(a);
+    else logits_kernel<T, VECS, false><<<grid, kThreads, 0, stream>>>(a);
+  }
 }
 
 template <class T>
@@ -207,7 +214,7 @@ void dispatch(const Logits& a, hipStream_t stream) {
 spt_status adjust_logits_dispatch(int32_t dtype, int64_t R, int64_t V, const void* logits, int64_t logits_stride,
                                   const spt_logit_rules* rules, void* out, int64_t out_stride, hipStream_t stream) {
   const Logits a{logits, out, logits_stride, out_stride, rules->allowed_stride, static_cast<int>(R), static_cast<int>(V),
-                 static_cast<int>(rules->sequences), rules->first, pattern_view(rules->seen), pattern_view(rules->tree),
+                 static_cast<int>(rules->sequences), 0, rules->first, pattern_view(rules->seen), pattern_view(rules->tree),
                  pattern_view(rules->bias), rules->bias ? static_cast<const float*>(rules->bias->vals) : nullptr, rules->drafts,
                  rules->repetition, rules->presence, rules->frequency, rules->allowed};
   if (dtype == SPT_F32) dispatch<float>(a, stream);

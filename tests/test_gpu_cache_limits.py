@@ -79,3 +79,25 @@ def test_pools_of_as_many_pages_as_one_may_have(pages):
     assert refs[-3:].tolist() == [1, 1, 1] and int(refs[5]) == 1
     del refs, cache
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("rows", [2 ** 22, 2 ** 23 + 5, 2 ** 24])
+def test_logits_of_as_many_rows_as_there_may_be(rows):
+    """More rows than workgroups of one launch, alone and as sequences of three."""
+    import paper_1804_10112_amd as spt
+    V = 3
+    logits = torch.randint(-8, 8, (rows, V), device="cuda").float()
+    tokens = torch.randint(0, V, (rows,), dtype=torch.int32, device="cuda")
+    out = torch.full_like(logits, 7.0)
+    presence = torch.arange(rows, device="cuda").remainder(5).float()
+    spt.spt_adjust_logits(logits, spt.LogitRules(presence=presence, drafts=tokens), out)
+    want = logits.clone()
+    want[torch.arange(rows, device="cuda"), tokens.long()] -= presence
+    assert torch.equal(out, want)
+    sequences = rows // 3
+    first = torch.arange(0, 3 * sequences + 1, 3, dtype=torch.int32, device="cuda")
+    out.fill_(7.0)
+    spt.spt_adjust_logits(logits, spt.LogitRules(first=first, presence=presence[:sequences].contiguous(), drafts=tokens), out)
+    way = torch.nn.functional.one_hot(tokens[:3 * sequences].long(), V).view(sequences, 3, V).cumsum(1).view(-1, V) > 0
+    want = logits[:3 * sequences] - way * presence[:sequences].repeat_interleave(3)[:, None]
+    assert torch.equal(out[:3 * sequences], want) and bool((out[3 * sequences:] == 7).all())
