@@ -27,10 +27,11 @@ struct Values {
   T v[Vec16<T>::n];
 };
 
-// x / d with 1 / d at hand: the product, corrected once by its remainder. Where that is none (infinities, d = 0), the product.
+// x / d with 1 / d at hand: the product, corrected once by its remainder. Where that is not finite (x or d is an infinity or NaN, d = 0,
+// 1 / d or the product is beyond the largest number, which the quotient need not be), the division.
 __device__ __forceinline__ float quotient(float x, float d, float by_d) {
   const float q = x * by_d, rest = __builtin_fmaf(-q, d, x);
-  return rest == rest ? __builtin_fmaf(rest, by_d, q) : q;
+  return fabsf(rest) < INFINITY ? __builtin_fmaf(rest, by_d, q) : x / d;
 }
 
 constexpr int kKept = 8;            // tokens of the sequence that a thread holds in registers; the others are read again for each segment
