@@ -288,9 +288,27 @@ __global__ void write_kernel(Cache c, int layer, const int32_t* __restrict__ fir
 
 // ---- compact ----------------------------------------------------------------------------------------------------------------
 
-// Drafted tokens that a row has and keeps.
-__device__ __forceinline__ int kept(const Cache& c, const Pattern& keep, int s, int drafts) {
-  return clamped(pattern_end(keep, s) - pattern_begin(keep, s), 0, drafts);
+// Entries of a row's list that name drafted tokens it has. The list ascends, so those that are none lie at its ends: a look at both ends,
+// and a search (halving, by every thread for itself) only where there are some.
+struct Kept {
+  int begin, count;
+};
+__device__ __forceinline__ Kept kept(const Pattern& keep, int s, int drafts) {
+  int begin = pattern_begin(keep, s), end = pattern_end(keep, s);
+  if (begin < end && (keep.crd[begin] < 0 || keep.crd[end - 1] >= drafts)) {
+    auto below = [&](int limit) {  // the first entry that is not below it
+      int lo = begin, hi = end;
+      while (lo < hi) {
+        const int mid = lo + ((hi - lo) >> 1);
+        if (keep.crd[mid] < limit) lo = mid + 1;
+        else hi = mid;
+      }
+      return lo;
+    };
+    const int from = below(0), to = below(drafts);
+    begin = from, end = to;
+  }
+  return {begin, clamped(end - begin, 0, drafts)};
 }
 
 // A thread owns 16 bytes of each token of the row (in one layer, K or V, and head) and moves them token after token, kBatch loads at a
@@ -303,7 +321,9 @@ __global__ void __launch_bounds__(kBlock) compact_move_kernel(Cache c, const int
   __shared__ int64_t from[kMoves], to[kMoves];  // -1: stays where it is
   const int s = blockIdx.x, vecs = c.width_bytes / 16;
   const Drafted d = drafted(first, s, INT32_MAX);
-  const int context = row_length(c, s) - d.count, begin = pattern_begin(keep, s), n = kept(c, keep, s, d.count);
+  const int context = row_length(c, s) - d.count;
+  const Kept k = kept(keep, s, d.count);
+  const int begin = k.begin, n = k.count;
   if (context < 0 || n == 0) return;
   int r = blockIdx.y * blockDim.x + threadIdx.x;
   const bool mine = r < c.layers * 2 * c.heads * vecs;
@@ -347,7 +367,7 @@ __global__ void compact_cut_kernel(Cache c, const int32_t* __restrict__ first, P
   const Drafted d = drafted(first, s, INT32_MAX);
   const int before = row_length(c, s), context = before - d.count;
   if (context < 0 || d.count == 0) return;
-  const int after = context + kept(c, keep, s, d.count);
+  const int after = context + kept(keep, s, d.count).count;
   release(c, s, pages_held(c, after), pages_held(c, before));
   if (lane_id() == 0) c.len[s] = after;
 }
