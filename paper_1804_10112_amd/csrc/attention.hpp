@@ -355,10 +355,17 @@ __device__ __forceinline__ float sum_of_row(float x) {
 }
 
 // One step of the softmax of 16 rows each: scores z (16 tokens each, 4q .. 4q+3 of a lane) become weights exp2(scale z - m). What is
-// held so far is rescaled, and m raised, only when a score passes m by more than 2^kSlack in weight: most steps leave it, the weights
-// stay below 2^kSlack (f16 holds 2^16), and m cancels in the result. scale > 0.
-constexpr float kSlack = 8;
-template <int COUNT, int NQ, int SUB, int TILES>
+// held so far is rescaled, and m raised, only when a weight would pass 2^kMost: most steps leave it, and m cancels in the result. It is
+// raised to 2^kBelow below the largest weight. scale > 0.
+// f16 holds 2^16, and below 2^-14 with fewer bits, below 2^-25 nothing, while the sum l keeps all: the largest weights lie between 2^11
+// and 2^15, so that only those less than 2^-25 of them lose bits. What is lost of a token is less than 2^-36 of the largest weight,
+// all together less than half a step of f16 in rows of 2^25 tokens whose values are alike. (With a largest weight of 1, tokens of 2^-26
+// were lost altogether, those of 2^-20 off by up to 3 %.) The other types have the range of 32 bits.
+template <class T>
+struct Weights {
+  static constexpr float kBelow = __is_same(T, f16) ? 11 : 0, kMost = __is_same(T, f16) ? 15 : 8;
+};
+template <class T, int COUNT, int NQ, int SUB, int TILES>
 __device__ __forceinline__ void softmax_step(f4 (&z)[COUNT][SUB], float scale, float (&m)[NQ], float (&l)[NQ], f4 (&o)[NQ][TILES]) {
   float top[COUNT];
   bool grown = false;
@@ -370,12 +377,12 @@ __device__ __forceinline__ void softmax_step(f4 (&z)[COUNT][SUB], float scale, f
 #pragma unroll
       for (int r = 0; r < 4; ++r) top[n] = fmaxf(top[n], z[n][u][r]);
     top[n] = max_of_row(top[n]) * scale;
-    grown |= top[n] > m[n] + kSlack;
+    grown |= top[n] > m[n] + Weights<T>::kMost;
   }
   if (__any(grown))
 #pragma unroll
     for (int n = 0; n < COUNT; ++n) {
-      const float high = fmaxf(m[n], top[n]), keep = exp2_of(m[n] - (high == -INFINITY ? 0 : high));
+      const float high = fmaxf(m[n], top[n] - Weights<T>::kBelow), keep = exp2_of(m[n] - (high == -INFINITY ? 0 : high));
       l[n] *= keep;
 #pragma unroll
       for (int d = 0; d < TILES; ++d) o[n][d] *= keep;
@@ -395,7 +402,7 @@ __device__ __forceinline__ void softmax_step(f4 (&z)[COUNT][SUB], float scale, f
 }
 
 // The weights of 32 tokens (16 of float32) as an operand. They are rounded to the values' type, which the matrix instruction takes:
-// half a step of it (2^-9 of a weight in bf16, 2^-12 in f16), no more than the rounding of the result; their sum l is not rounded.
+// off by at most half a step of it (2^-8 of a weight in bf16, 2^-11 in f16), as the result is; their sum l is not rounded.
 template <class T>
 __device__ __forceinline__ i4 weights(const f4* z) {
   if constexpr (sizeof(T) == 4) {

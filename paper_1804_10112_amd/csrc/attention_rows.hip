@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
             for (int w = 0; w < 2; ++w) sight[n][w] = row_sight(a, at.q, row0 + mine + 64 * n + i, base + 32 * w) & ~gone[w];
             hide(z[n], sight[n]);
           }
-        softmax_step(z, a.scale, m, l, o);
+        softmax_step<T>(z, a.scale, m, l, o);
         i4 p[NQ][kSub / 2];
 #pragma unroll
         for (int w = 0; w < kSub / 2; ++w)

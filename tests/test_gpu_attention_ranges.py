@@ -1,0 +1,55 @@
+"""Attention at the ends of the numbers' range: weights far below the largest one."""
+import math
+
+import pytest
+import torch
+
+from cache_util import DTYPES, HALF_STEP, HostCache, gpu_attention
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [(1, 2), (20, 4), (70, 4)]                                     # drafts, query heads a head: tiles of 16, 64, 128 rows
+
+
+def _rows_of_one_score(tokens, q_heads, width, dtype):
+    q = torch.zeros(tokens, q_heads, width, dtype=DTYPES[dtype])
+    q[:, :, 0] = 1
+    return q
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("drafts,group", SHAPES)
+@pytest.mark.parametrize("spread_out", [True, False])
+@pytest.mark.parametrize("gap", [8.0, 14.0, 17.0, 18.0])
+def test_many_tokens_far_below_one(dtype, drafts, group, spread_out, gap):
+    """One token with a score of `gap`, 3000 of score 0: each of those weighs exp(-gap), up to 26 powers of two less. Its value is 0,
+    so the result is the others' contribution alone. 40 sequences of 8 heads: a wave goes through hundreds of tokens after that one.
+
+    A weight is rounded once to the values' type (half a step of it); in f16 one that is less than 2^-25 of the largest falls below
+    the least normal number and is then off by at most 2^-36 of the largest. The exponential's argument is rounded to 32 bits where
+    it is up to 38 (|gap| / ln 2 and 11), half a step of 2^-18, and its value to a step. Each sum of n positive numbers in 32 bits is off
+    by (n - 1) 2^-24 of itself at most (exp(-17) added to 1 is less than half a step of it, and lost). The result is rounded once."""
+    length, rows, heads, width = 3000, 40, 8, 8
+    host = HostCache([length + drafts] * rows, 64, heads, width, dtype, poison=False, seed=drafts)
+    host.K.zero_()
+    host.V.abs_().add_(0.5)
+    for s in range(rows):
+        for h in range(heads):
+            p, o = host.slot(s, (331 * s + 97 * h) % length if spread_out else 0)
+            host.K[0, p, o, h, 0], host.V[0, p, o, h] = gap, 0
+    out, lse = gpu_attention(host.device(), 0, [drafts] * rows, None, _rows_of_one_score(rows * drafts, group * heads, width, dtype), 1.0)
+    pages = torch.tensor(host.table)[:, :host.held(length + drafts)]
+    values = host.V[0][pages].reshape(rows, -1, heads, width)[:, :length + drafts].double()
+    others = values.cumsum(1)[:, length:].flatten(0, 1).repeat_interleave(group, 1)     # of the tokens that each draft sees
+    seen = torch.arange(length, length + drafts, dtype=torch.float64).repeat(rows)[:, None, None]
+    small = math.exp(-gap)
+    total = 1 + seen * small
+    want = small * others / total
+    h = HALF_STEP[dtype]
+    exact = 2.0 ** -18 + 2.0 ** -22 + (length + drafts + 64) * 2.0 ** -24
+    weights = exact + (0 if dtype == "f32" else h)
+    lost = 2.0 ** -36 * others + 2.0 ** -25 if dtype == "f16" else 0
+    error, bound = (out.double() - want).abs(), want * (2 * weights + h) + lost
+    assert bool((error <= bound).all()), f"{float((error / bound).max())} times the bound"
+    want_lse = gap + torch.log(total[:, :, 0])
+    assert bool(((lse.double() - want_lse).abs() <= exact + 2.0 ** -23 * want_lse).all())
