@@ -398,8 +398,8 @@ spt_status cache_attention_dispatch(const spt_cache* cache, int32_t layer, const
   Workspace w(ws, cache_attention_workspace(cache, q_heads));
   Part* part = w.take<Part>(kMostGroups);
   float* partial = w.take<float>(0);
-  // a scale of 0 becomes one that makes 0 of every score as well, but hidden ones stay -infinity
-  const float factor = scale == 0 ? 1e-38f : fabsf(scale) * 1.4426950408889634f;
+  // a scale of 0 becomes the smallest number, with which hidden scores stay -infinity and the largest ones are 5e-7
+  const float factor = scale == 0 ? __FLT_DENORM_MIN__ : fabsf(scale) * 1.4426950408889634f;
   const Attention a{cache_view(cache), layer, total, q_heads, q_heads / cache->heads, divisor(q_heads / cache->heads), first, pattern_view(tree),
                     static_cast<const char*>(q), static_cast<char*>(out), lse, q_token_stride * b, q_head_stride * b,
                     out_token_stride * b, out_head_stride * b, factor, scale < 0, part, partial};

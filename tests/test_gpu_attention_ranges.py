@@ -1,4 +1,4 @@
-"""Attention at the ends of the numbers' range: weights far below the largest one."""
+"""Attention at the ends of the numbers' range: weights far below the largest one, scores with a scale of 0."""
 import math
 
 import pytest
@@ -53,3 +53,21 @@ def test_many_tokens_far_below_one(dtype, drafts, group, spread_out, gap):
     assert bool((error <= bound).all()), f"{float((error / bound).max())} times the bound"
     want_lse = gap + torch.log(total[:, :, 0])
     assert bool(((lse.double() - want_lse).abs() <= exact + 2.0 ** -23 * want_lse).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("drafts,q_heads", SHAPES)
+def test_a_scale_of_zero_weighs_scores_of_any_size_alike(dtype, drafts, q_heads):
+    """z = 0 * score = 0 for every finite score, 3e37 too."""
+    host = HostCache([200 + drafts], 16, 1, 64, dtype, poison=False, seed=3)
+    host.K[..., 0] = torch.where(torch.rand(host.K.shape[:-1]) < 0.5, 1e19, -1e19).to(DTYPES[dtype])
+    q = _rows_of_one_score(drafts, q_heads, 64, dtype) * 3e18
+    out, lse = gpu_attention(host.device(), 0, [drafts], None, q, 0.0)
+    pages = torch.tensor(host.table[0][:host.held(200 + drafts)])
+    values = host.V[0][pages, :, 0].reshape(-1, 64)[:200 + drafts].double()
+    seen = torch.arange(201, 201 + drafts, dtype=torch.float64)
+    want = values.cumsum(0)[200:] / seen[:, None]
+    spread = values.abs().cumsum(0)[200:] / seen[:, None]
+    bound = (HALF_STEP[dtype] * want.abs() + (64 + 270) * 2.0 ** -23 * spread)[:, None]
+    assert bool(((out.double() - want[:, None]).abs() <= bound).all())
+    assert bool(((lse.double() - torch.log(seen)[:, None]).abs() <= (64 + 270) * 2.0 ** -23).all())
