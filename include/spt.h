@@ -550,8 +550,9 @@ spt_status spt_cache_fork(const spt_cache* c, int64_t n, const int32_t* parents,
  * they are below 2^-25.
  * q, out: T x q_heads x width with the strides given (elements, multiples of 16 bytes; pointers 16-byte aligned),
  * T <= 2^24, T * (q_heads/heads) < 2^31 - 256; q_heads a multiple of heads; q and out may be one array with the
- * same strides; lse (may be NULL): float, T x q_heads. The size of the workspace depends neither on lengths nor on
- * T. The same call gives the same bits. Workspace: SPT_CACHE_ATTENTION.
+ * same strides; scale: -2^127 .. 2^127; lse (may be NULL): float, T x q_heads. The same call gives the same
+ * bits. Workspace: SPT_CACHE_ATTENTION, 9 to 68 MB by width and dtype (SPT_F16, SPT_BF16 of 128 values: 68); its
+ * size depends neither on lengths nor on T.
  */
 spt_status spt_cache_attention(const spt_cache* c, int32_t layer, const int32_t* first, int64_t T,
                                const spt_tensor* tree, const void* q, int32_t q_heads, int64_t q_token_stride,

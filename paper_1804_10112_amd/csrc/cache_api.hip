@@ -24,6 +24,9 @@ spt_status adjust_logits_dispatch(int32_t dtype, int64_t R, int64_t V, const voi
 constexpr int64_t kMaxRows = 1 << 20, kMaxTokens = 1 << 24, kMaxForks = 1 << 16, kMaxStride = int64_t(1) << 40, kMaxInPage = int64_t(1) << 33,
                   kMaxColumns = 1 << 27;
 
+// Of a scale: times log2(e) it is still a number. With an infinity scores of 0 would become NaN, with NaN hidden ones too.
+constexpr float kMostScale = 0x1p127f;
+
 static bool narrow_type(int32_t dtype, const char* what) {
   if (dtype == SPT_F32 || dtype == SPT_F16 || dtype == SPT_BF16) return true;
   if (dtype == SPT_F64)
@@ -191,6 +194,8 @@ spt_status spt_cache_attention(const spt_cache* c, int32_t layer, const int32_t*
   if (q_heads < 1 || q_heads > 65535 || q_heads % c->heads != 0)
     return fail(SPT_ERR_INVALID_ARG, "cache_attention: q_heads %d is not a multiple of the cache's %d heads, up to 65535", q_heads,
                 c->heads);
+  if (!(scale >= -kMostScale && scale <= kMostScale))
+    return fail(SPT_ERR_INVALID_ARG, "cache_attention: scale %g is not a number from -2^127 to 2^127", static_cast<double>(scale));
   if (T * (q_heads / c->heads) >= INT32_MAX - 256)
     return fail(SPT_ERR_UNSUPPORTED, "cache_attention: %lld tokens of %d query heads for each head of K", (long long)T,
                 q_heads / c->heads);

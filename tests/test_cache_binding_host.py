@@ -148,3 +148,18 @@ def test_descriptors_of_tensors_on_several_devices_are_refused():
                   dict(bias=spt.DeviceCSR(ints(-1, 0, 1), ints(-1, 0), 2, OnDevice(torch.zeros(1), -1)))):
         with pytest.raises(spt.SptError):
             spt.LogitRules(first=ints(0, 0, 1), **given)
+
+
+@pytest.mark.parametrize("scale,status", [(float("nan"), 1), (float("inf"), 1), (-float("inf"), 1), (3e38, 1), (-3e38, 1), (2.0 ** 127, 0),
+                                          (-2.0 ** 127, 0), (0.0, 0), (1e-45, 0)])
+def test_scales_that_no_score_can_be_multiplied_with_are_refused(scale, status):
+    import ctypes
+    c = spt.binding.SptCache()
+    for name, value in dict(dtype=spt.SPT_BF16, layers=1, heads=2, width=64, page=16, rows=0, row_pages=2, pages=0, layer_stride=0,
+                            page_stride=2048, slot_stride=128, head_stride=64).items():
+        setattr(c, name, value)
+    p, lib = ctypes.addressof(c), spt.lib()
+    need = lib.spt_cache_workspace_bytes(spt.SPT_CACHE_ATTENTION, p, 4)
+    # no rows: a call that is accepted does nothing
+    assert lib.spt_cache_attention(p, 0, None, 0, None, None, 4, 256, 64, scale, None, 256, 64, None, 0x10000, need, None) == status
+    assert status == 0 or "scale" in spt.spt_last_error()
