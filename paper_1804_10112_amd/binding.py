@@ -518,9 +518,12 @@ class DeviceCache:
 
     def __init__(self, K, V, table, length, refs):
         _use_torch()
-        if K.dim() != 5 or K.shape != V.shape or K.stride() != V.stride() or K.dtype != V.dtype:
+        if K.dim() != 5 or K.shape != V.shape or K.dtype != V.dtype:
             _invalid("K and V must be alike: (layers, pages, slots of a page, heads, width)")
-        if K.stride(4) != 1:
+        strides = [_stride(K, d) for d in range(4)]
+        if strides != [_stride(V, d) for d in range(4)]:
+            _invalid("K and V must have the same strides")
+        if K.stride(4) != 1 or V.stride(4) != 1:
             _invalid("the values of a head must be contiguous")
         if table.dim() != 2:
             _invalid("table must be (rows, pages of a row)")
@@ -528,7 +531,7 @@ class DeviceCache:
         c.dtype = _dtype_code(K.dtype)
         c.layers, c.pages, c.page, c.heads, c.width = K.shape
         c.rows, c.row_pages = table.shape
-        c.layer_stride, c.page_stride, c.slot_stride, c.head_stride = (_stride(K, d) for d in range(4))
+        c.layer_stride, c.page_stride, c.slot_stride, c.head_stride = strides
         c.K, c.V = K.data_ptr(), V.data_ptr()
         c.table, c.len, c.refs = _i32(table, 0, "table"), _i32(length, c.rows, "len"), _i32(refs, c.pages, "refs")
         self.K, self.V, self.table, self.len, self.refs = K, V, table, length, refs

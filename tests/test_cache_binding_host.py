@@ -163,3 +163,13 @@ def test_scales_that_no_score_can_be_multiplied_with_are_refused(scale, status):
     # no rows: a call that is accepted does nothing
     assert lib.spt_cache_attention(p, 0, None, 0, None, None, 4, 256, 64, scale, None, 256, 64, None, 0x10000, need, None) == status
     assert status == 0 or "scale" in spt.spt_last_error()
+
+
+def test_strides_of_axes_of_one_do_not_count():
+    """torch leaves them as they come: K of a pool with the layers behind the pages, V of one of its own."""
+    K, V = torch.zeros(4, 1, 16, 2, 64).transpose(0, 1), torch.zeros(1, 4, 16, 2, 64)
+    assert K.stride() != V.stride()
+    cache = spt.DeviceCache(K, V, i32(0, 1, 2, 3).view(2, 2), i32(0, 0), i32(0, 0, 0, 0))
+    assert (cache.c.layer_stride, cache.c.page_stride, cache.c.slot_stride, cache.c.head_stride) == (0, 2048, 128, 64)
+    with pytest.raises(spt.SptError):
+        spt.DeviceCache(K.expand(2, -1, -1, -1, -1), V.repeat(2, 1, 1, 1, 1), i32(0, 1, 2, 3).view(2, 2), i32(0, 0), i32(0, 0, 0, 0))
