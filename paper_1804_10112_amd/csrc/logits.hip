@@ -34,15 +34,17 @@ __device__ __forceinline__ float quotient(float x, float d, float by_d) {
   return fabsf(rest) < INFINITY ? __builtin_fmaf(rest, by_d, q) : x / d;
 }
 
-constexpr int kKept = 8;            // tokens of the sequence that a thread holds in registers; the others are read again for each segment
+// Tokens of the sequence that a thread holds in registers; those behind the first 4096 are read again for each segment. 64 rows of 128 000
+// logits in bf16, tokens seen: 1000 13 us, 4000 13, 8000 16, 30 000 37, 100 000 123.
+constexpr int kKept = 8;
 constexpr int kNowhere = -(1 << 30);  // below every segment
 
 // A workgroup takes segments of a row, VECS times 16 bytes a thread, counted from where the row is aligned: blockIdx.y, blockIdx.y +
 // gridDim.y, .. In LDS lie the counts of a segment's columns and their biases: integer counts and unique biases, so nothing depends on an
 // order. The sequence's tokens are read at once, into registers, and each segment picks its own; the logits of the next segment are
 // under way while one is counted. A thread clears the counts that it has read, so a segment takes two barriers. Bound: the logits' bytes,
-// 256 rows of 128 000 in bf16 with biases and masks 38 us, 3.7 TB/s; as many workgroups as run at once (four of 512 threads to a compute
-// unit): with half as many 60 us, with twice as many 46, with longer segments 55; and one row of 32 000 takes 4.3.
+// 256 rows of 128 000 in bf16 with biases and masks 38 us, 3.7 TB/s (in f32 61, 4.5); as many workgroups as run at once (four of 512 threads to a compute
+// unit): with half as many 60 us, with twice as many 46, with longer segments 55; and one row of 32 000 takes 4.4.
 template <class T, int VECS, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 8) logits_kernel(Logits a) {
   constexpr int n = Vec16<T>::n, kSegment = kThreads * VECS * n;
