@@ -544,7 +544,8 @@ spt_status spt_cache_fork(const spt_cache* c, int64_t n, const int32_t* parents,
  *   z_t = scale * sum_d q(i,h,d) K(t, h / (q_heads/heads), d),  p_t = exp(z_t) / sum of exp(z) over the tokens seen,
  *   out(i,h,:) = sum_t p_t V(t, h / (q_heads/heads), :),        lse(i,h) = ln(sum of exp(z)).
  * A token that sees nothing (or only scores of -infinity) gets out = 0 and lse = -infinity. What a token
- * does not see does not reach it, infinities and NaNs in K and V included. Scores, sums and out are held in
+ * does not see does not reach it, infinities and NaNs in K and V included. (A score beyond 2^127 counts as an
+ * infinity.) Scores, sums and out are held in
  * 32 bits; SPT_F16 and SPT_BF16 multiply in matrix instructions on values of that type, for which the weights
  * exp(z) / exp(max) are rounded to it: by half a step (2^-11, 2^-8 of a weight), in SPT_F16 by up to 2^-36 where
  * they are below 2^-25.

@@ -66,6 +66,7 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
     }
     f4 o[NQ][kTiles];
     float m[NQ], l[NQ];
+    bool vast = false;
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
       m[n] = -INFINITY;
@@ -134,7 +135,7 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
       if (!all)
 #pragma unroll
         for (int n = 0; n < NQ; ++n) hide(z[n], &sight[n]);
-      softmax_step<T>(z, a.scale, m, l, o);
+      softmax_step<T>(z, a.scale, m, l, o, vast);
       i4 p[NQ];
 #pragma unroll
       for (int n = 0; n < NQ; ++n) p[n] = weights<T>(z[n]);

@@ -367,8 +367,13 @@ template <class T>
 struct Weights {
   static constexpr float kBelow = __is_same(T, f16) ? 11 : 0, kMost = __is_same(T, f16) ? 15 : 8;
 };
+// A weight's exponent is rounded once, in an fma; m is a product that was rounded before. From 2^22 on that rounding is no longer small (at
+// 2^30 the largest weight could be 2^32 as well as 2^-32), and m - kBelow not what it says: once an m is so large (vast, alike in all
+// lanes) the products are rounded in the exponents too, so that the largest is 0.
+constexpr float kVast = 1 << 22;
 template <class T, int COUNT, int NQ, int SUB, int TILES>
-__device__ __forceinline__ void softmax_step(f4 (&z)[COUNT][SUB], float scale, float (&m)[NQ], float (&l)[NQ], f4 (&o)[NQ][TILES]) {
+__device__ __forceinline__ void softmax_step(f4 (&z)[COUNT][SUB], float scale, float (&m)[NQ], float (&l)[NQ], f4 (&o)[NQ][TILES], bool& vast) {
+  const float most = vast ? 0 : Weights<T>::kMost;  // which the sum with a vast m would round
   float top[COUNT];
   bool grown = false;
 #pragma unroll
@@ -379,17 +384,30 @@ __device__ __forceinline__ void softmax_step(f4 (&z)[COUNT][SUB], float scale, f
 #pragma unroll
       for (int r = 0; r < 4; ++r) top[n] = fmaxf(top[n], z[n][u][r]);
     top[n] = max_of_row(top[n]) * scale;
-    grown |= top[n] > m[n] + Weights<T>::kMost;
+    grown |= top[n] > m[n] + most;
   }
-  if (__any(grown))
+  if (__any(grown)) {
+    bool large = false;
 #pragma unroll
     for (int n = 0; n < COUNT; ++n) {
-      const float high = fmaxf(m[n], top[n] - Weights<T>::kBelow), keep = exp2_of(m[n] - (high == -INFINITY ? 0 : high));
+      const float below = fabsf(top[n]) < kVast ? Weights<T>::kBelow : 0;
+      const float high = fmaxf(m[n], top[n] - below), keep = exp2_of(m[n] - (high == -INFINITY ? 0 : high));
       l[n] *= keep;
 #pragma unroll
       for (int d = 0; d < TILES; ++d) o[n][d] *= keep;
       m[n] = high;
+      large |= fabsf(high) >= kVast && high != -INFINITY;
     }
+    vast |= __any(large) != 0;
+  }
+  if (vast) {  // here, rounded (no fma of it and the difference below), with a scale of 1 below
+#pragma clang fp contract(off)
+#pragma unroll
+    for (int n = 0; n < COUNT; ++n)
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) z[n][u] *= scale;
+    scale = 1;
+  }
 #pragma unroll
   for (int n = 0; n < COUNT; ++n) {
     const float zero = m[n] == -INFINITY ? 0 : m[n];

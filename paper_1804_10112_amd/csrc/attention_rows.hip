@@ -102,6 +102,7 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
     finish_queries<T, FULL>(a, qf);
     f4 o[NQ][kTiles];
     float m[NQ], l[NQ];
+    bool vast = false;
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
       m[n] = -INFINITY;
@@ -150,7 +151,7 @@ __global__ void __launch_bounds__(kBlock, (groups_of<ROW_BYTES, sizeof(T)>() / 2
             for (int w = 0; w < 2; ++w) sight[n][w] = row_sight(a, at.q, row0 + mine + 64 * n + i, base + 32 * w) & ~gone[w];
             hide(z[n], sight[n]);
           }
-        softmax_step<T>(z, a.scale, m, l, o);
+        softmax_step<T>(z, a.scale, m, l, o, vast);
         i4 p[NQ][kSub / 2];
 #pragma unroll
         for (int w = 0; w < kSub / 2; ++w)

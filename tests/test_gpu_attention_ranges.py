@@ -71,3 +71,55 @@ def test_a_scale_of_zero_weighs_scores_of_any_size_alike(dtype, drafts, q_heads)
     bound = (HALF_STEP[dtype] * want.abs() + (64 + 270) * 2.0 ** -23 * spread)[:, None]
     assert bool(((out.double() - want[:, None]).abs() <= bound).all())
     assert bool(((lse.double() - torch.log(seen)[:, None]).abs() <= (64 + 270) * 2.0 ** -23).all())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("drafts,q_heads", SHAPES)
+@pytest.mark.parametrize("sign", [1, -1])
+def test_finite_scores_of_any_size(dtype, drafts, q_heads, sign):
+    """One token's score is the largest by far more than any rounding, and as large as the type lets it be (keys of the type's lowest number
+    among them): it has all the weight, so the result is its value and lse its score, off by its rounding in 32 bits.
+
+    The score is a product of two numbers, exact or rounded once, times the scale; ln and log2 cost a few roundings more. Its weight w
+    is rounded to the type once (half a step h; the sum of weights is w itself), the result w V / w once, and in 32 bits three times."""
+    h = 0.0 if dtype == "f32" else HALF_STEP[dtype]
+    largest = torch.finfo(DTYPES[dtype]).max
+    for size in [1e3, 3e4, 6e4, largest] + ([] if dtype == "f16" else [1.1e7, 3e8, 7.7e9, 1e20, 1.2345e31, 3e37]):
+        for factor in (0.37, 1.0, 60000.0 if dtype == "f16" else 1.9):
+            # the other tokens' keys are a tenth of it: their scores less than half of the largest, or negative
+            host = HostCache([300 + drafts], 16, 1, 64, dtype, poison=False, seed=3)
+            q = _rows_of_one_score(drafts, q_heads, 64, dtype) * factor
+            host.K.zero_()
+            host.K[..., 0] = -sign * size
+            host.K[0, :, ::2, 0, 0] = sign * size / 10
+            best = 171                                                  # an odd slot of its page
+            p, o = host.slot(0, best)
+            host.K[0, p, o, 0, 0] = sign * size
+            scale = sign * 0.9
+            key, query = host.K[0, p, o, 0, 0].double(), q[0, 0, 0].double()
+            score = float(key * query * torch.tensor(scale, dtype=torch.float32).double())
+            if abs(score) * 1.4427 > 3e38:
+                continue
+            out, lse = gpu_attention(host.device(), 0, [drafts], None, q, scale)
+            value = host.V[0, p, o].double()
+            assert bool(((out.double() - value).abs() <= (2 * h + h * h + 2.0 ** -22) * value.abs()).all()), (size, factor)
+            assert bool(((lse.double() - score).abs() <= 8 * 2.0 ** -24 * abs(score)).all()), (size, factor)
+
+
+def test_all_scores_as_low_as_they_can_be():
+    """Keys of the lowest number everywhere: all weigh alike, whatever their score."""
+    for dtype in ("bf16", "f32"):
+        for drafts, q_heads in SHAPES:
+            host = HostCache([200 + drafts], 16, 1, 64, dtype, poison=False, seed=3)
+            host.K.zero_()
+            host.K[..., 0] = torch.finfo(DTYPES[dtype]).min
+            q = _rows_of_one_score(drafts, q_heads, 64, dtype)
+            out, lse = gpu_attention(host.device(), 0, [drafts], None, q, 0.3)
+            pages = torch.tensor(host.table[0][:host.held(200 + drafts)])
+            values = host.V[0][pages, :, 0].reshape(-1, 64)[:200 + drafts].double()
+            seen = torch.arange(201, 201 + drafts, dtype=torch.float64)
+            want = values.cumsum(0)[200:] / seen[:, None]
+            spread = values.abs().cumsum(0)[200:] / seen[:, None]
+            bound = (HALF_STEP[dtype] * want.abs() + (64 + 270) * 2.0 ** -23 * spread)[:, None]
+            assert bool(((out.double() - want[:, None]).abs() <= bound).all()), dtype
+            assert bool((lse < -1e37).all() and torch.isfinite(lse).all())
