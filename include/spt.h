@@ -545,10 +545,9 @@ spt_status spt_cache_fork(const spt_cache* c, int64_t n, const int32_t* parents,
  *   out(i,h,:) = sum_t p_t V(t, h / (q_heads/heads), :),        lse(i,h) = ln(sum of exp(z)).
  * A token that sees nothing (or only scores of -infinity) gets out = 0 and lse = -infinity. What a token
  * does not see does not reach it, infinities and NaNs in K and V included. (A score beyond 2^127 counts as an
- * infinity.) Scores, sums and out are held in
- * 32 bits; SPT_F16 and SPT_BF16 multiply in matrix instructions on values of that type, for which the weights
- * exp(z) / exp(max) are rounded to it: by half a step (2^-11, 2^-8 of a weight), in SPT_F16 by up to 2^-36 where
- * they are below 2^-25.
+ * infinity.) Scores, sums and out are held in 32 bits; SPT_F16 and SPT_BF16 multiply in matrix instructions on
+ * values of that type, for which the weights exp(z) / exp(max) are rounded to it: by half a step (2^-11, 2^-8 of
+ * a weight), in SPT_F16 by up to 2^-36 where they are below 2^-25.
  * q, out: T x q_heads x width with the strides given (elements, multiples of 16 bytes; pointers 16-byte aligned),
  * T <= 2^24, T * (q_heads/heads) < 2^31 - 256; q_heads a multiple of heads; q and out may be one array with the
  * same strides; scale: -2^127 .. 2^127; lse (may be NULL): float, T x q_heads. The same call gives the same

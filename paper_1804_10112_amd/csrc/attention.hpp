@@ -14,7 +14,7 @@
 // which of them end first, took 4 % longer on a decoding batch and 30 % longer on trees, each having its own start and parts.
 //
 // What bounds it: the reading of K and V, up to some 250 rows a sequence (1.33 GB of a decoding batch of 64 rows: 265 us and 5 for the
-// joining, 4.9 TB/s, what a large copy reaches), the matrix products and the softmax beyond (chunks of 1024 tokens: 584 TFLOP/s, half of a
+// joining, 4.9 TB/s, what a large copy reaches), the matrix products and the softmax beyond (chunks of 1024 tokens: 579 TFLOP/s, half of a
 // large matrix product's), and in small calls the way to the first load: some 8 us in a workgroup, 4 for the joining.
 #pragma once
 #include "cache.hpp"

@@ -2,8 +2,8 @@
 //
 // The four waves of a workgroup take 16 rows of each 64 of a tile and the same tokens, 64 a step: K and V come to LDS once for all of them, two
 // steps' worth of it; the loads of the next step or two are under way, in registers, meanwhile.
-// A tree of 16 drafted tokens (64 rows) over 100 000 tokens, 205 MB: 56 us and 9 for the joining; waves wait for half of it. Chunks of 1024
-// tokens: 170 us and 17; the matrix units are busy for 29 % of the 170, the vector units for 51 %, LDS for 22 %, of which conflicts are
+// A tree of 16 drafted tokens (64 rows) over 100 000 tokens, 205 MB: 57 us and 9 for the joining; waves wait for half of it. Chunks of 1024
+// tokens: 172 us and 17; the matrix units are busy for 28 % of the 172, the vector units for 50 %, LDS for 22 %, of which conflicts are
 // less than a thousandth (by counters). Measured without gain: half of the tokens for twice the rows of a wave (reads of LDS halved), the
 // next tile's loads under way while one is written, higher priority for waves that multiply.
 #include "attention.hpp"

@@ -1,7 +1,7 @@
 // The pages of a cache: rows that are extended, written, compacted, cut and forked. All of it is integer work on the table and
 // copies of whole slots, so results do not depend on the order in which workgroups run. Nearly all of these kernels take what a launch and
 // a few dependent loads take (1.3 to 5 us); copies move 16 bytes a lane: 56 forked rows whose last pages are copied in 4 layers, 27 MB
-// read and written, 16.5 us.
+// read and written, 16.7 us.
 #include "cache.hpp"
 
 namespace spt {
@@ -313,8 +313,8 @@ __device__ __forceinline__ Kept kept(const Pattern& keep, int s, int drafts) {
 
 // A thread owns 16 bytes of each token of the row (in one layer, K or V, and head) and moves them token after token, kBatch loads at a
 // time: the kept ones ascend, so a slot that is written was read before and is not read again. Where the tokens lie the workgroup
-// finds out first, kMoves of them at a time. 48 rows that keep a third of up to 64 tokens in 4 layers: 8.8 us, token after token with its
-// lookups 17. (Without a look at the lists' ends, which has to come before the length that is cut to, 8.3, and 2.8 instead of 3.6 for the cut.)
+// finds out first, kMoves of them at a time. 48 rows that keep a third of up to 64 tokens in 4 layers: 8.6 us, token after token with its
+// lookups 17. (Without a look at the lists' ends, which has to come before the length that is cut to, 8.3, and 2.8 instead of 3.2 for the cut.)
 constexpr int kMoves = kBlock, kBatch = 8;
 typedef int Bytes16 __attribute__((ext_vector_type(4)));
 __global__ void __launch_bounds__(kBlock) compact_move_kernel(Cache c, const int32_t* __restrict__ first, Pattern keep) {
