@@ -368,7 +368,7 @@ struct Weights {
   static constexpr float kBelow = __is_same(T, f16) ? 11 : 0, kMost = __is_same(T, f16) ? 15 : 8;
 };
 // A weight's exponent is rounded once, in an fma; m is a product that was rounded before. From 2^22 on that rounding is no longer small (at
-// 2^30 the largest weight could be 2^32 as well as 2^-32), and m - kBelow not what it says: once an m is so large (vast, alike in all
+// 2^30 the largest weight could be 2^64 as well as 2^-64), and m - kBelow not what it says: once an m is so large (vast, alike in all
 // lanes) the products are rounded in the exponents too, so that the largest is 0.
 constexpr float kVast = 1 << 22;
 template <class T, int COUNT, int NQ, int SUB, int TILES>
